@@ -103,7 +103,9 @@ enum {
   SPARQ_ERR_EMPTY_SEQ = 2,     /* decode of a sequence with S_b = 0: zeros written */
   SPARQ_ERR_IDX_TRUNCATED = 4, /* min(k_b, S_b) exceeded idx_stride: idx_out truncated */
   SPARQ_ERR_BAD_SEQ_LEN = 8,   /* seq_lens[b] outside [0, S_max]: clamped */
-  SPARQ_ERR_INTERNAL = 16      /* a consistency check inside a kernel failed (a defect of the library): results invalid */
+  SPARQ_ERR_INTERNAL = 16,     /* a consistency check inside a kernel failed (a defect of the library): results invalid */
+  SPARQ_ERR_BAD_ROWS = 32,     /* paged calls: a row count outside [0, n], or rows outside the packed buffers: that sequence has no rows */
+  SPARQ_ERR_BAD_PAGE = 64      /* paged calls: a page id outside the pool (see the calls) */
 };
 
 typedef struct {
@@ -276,6 +278,101 @@ const char* sparq_decode_plan(const sparq_shape* shape);
  * sparq_workspace_bytes of such a build includes the room.  Host only. */
 int sparq_stage_clocks(const sparq_shape* shape, size_t* offset_bytes, int32_t* n_workgroups,
                        int32_t* stamps_per_workgroup);
+
+/*
+ * ---- The paged cache: many new tokens at once, in 16 or 8 bits ----
+ *
+ * A pool of pages [n_pages, H_kv, page_size, d_h] for K and one for V; the positions i page_size .. (i + 1) page_size - 1 of
+ * sequence b stand in page page_table[b, i].  A contiguous cache is such a pool too: K and V [B, H_kv, S_max, d_h] are B pages of
+ * S_max positions.  The page table and the lengths are the caller's, nothing here writes them: seq_lens[b] counts the rows
+ * of the call, so that row t of the n_b rows of sequence b stands at position seq_lens[b] - n_b + t.  An append and the
+ * attention of the same rows are given the same lengths; both may run again with the same outcome.
+ *
+ * 8-bit pages hold d_h codes and one fp32 scale per row (position and KV head), and a code stands for code * scale.  A row x is
+ * written with a = max |x| (at least 2^-60, at most 2^100), scale = a / q and code = x * (q / a) rounded to the nearest code, ties to
+ * even, all in fp32; q is 127 (int8) or 448 (e4m3, the OCP format without infinities).  So a value is off by at most scale / 2
+ * (int8), or by 1 part in 16 or scale / 1024 (e4m3).  A row that holds an infinity or NaN gets the scale NaN and codes 0: it is
+ * read as NaN whole.  Scales that other programs write lie between 2^-70 (smaller ones are taken as that) and 2^96.
+ */
+typedef enum { SPARQ_PAGES_16 = 0, SPARQ_PAGES_I8 = 1, SPARQ_PAGES_E4M3 = 2 } sparq_page_type;
+
+enum {
+  SPARQ_FLAG_PAGED_ALL = 1u << 0   /* not causal: every row sees all positions 0 .. seq_lens[b] - 1 */
+};
+
+typedef struct {
+  int32_t B, H, H_kv, d_h;   /* d_h 64, 128 or 256 */
+  int32_t page_size;         /* positions per page, a multiple of 16 */
+  int32_t n_pages;           /* pages of the pool */
+  int32_t max_pages;         /* entries per row of the page table; max_pages * page_size < 2^31 */
+  int32_t dtype;             /* sparq_dtype of rows, queries and outputs, and of 16-bit pages */
+  int32_t page_type;         /* sparq_page_type */
+  uint32_t flags;
+  int32_t window;            /* w > 0: a row at position p sees only positions > p - w; 0: no window */
+  int32_t S_bound;           /* 0, or the caller's bound on the lengths in this call, at most max_pages * page_size (which it is 0
+                              * for): the attention's work is divided for lengths up to it */
+} sparq_paged_shape;
+
+typedef struct {
+  void* K;                   /* device [n_pages, H_kv, page_size, d_h] */
+  void* V;
+  float* K_scale;            /* device [n_pages, H_kv, page_size]; 8-bit pages only (ignored otherwise) */
+  float* V_scale;
+  const int32_t* page_table; /* device [B, max_pages] */
+  const int32_t* seq_lens;   /* device [B], the rows of the call included */
+} sparq_paged_cache;
+
+/* Which rows a call is about.  Row t of sequence b is found at base + b * strides.seq + head * strides.head + t * strides.row
+ * (elements), or with row_start at base + head * strides.head + (row_start[b] + t) * strides.row: sequences of different lengths
+ * packed one behind the other.  Rows that belong to no sequence, and those from n_b on, are neither read nor written. */
+typedef struct {
+  int32_t n;                 /* the most rows that a sequence has in this call (>= 1) */
+  int32_t n_rows;            /* with row_start: rows in the packed buffers; otherwise ignored */
+  const int32_t* n_per_seq;  /* device [B], rows of each sequence (0 .. n), or NULL: n everywhere */
+  const int32_t* row_start;  /* device [B + 1] or NULL; row_start[b + 1] - row_start[b] (0 .. n) is sequence b's count.  Not both. */
+} sparq_rows;
+
+typedef struct { int64_t seq, head, row; } sparq_strides;   /* elements, multiples of 8; channels are contiguous */
+
+/* Bytes of device workspace that the paged calls need for calls of up to n rows per sequence (>= 64 KiB, initialised once with
+ * sparq_workspace_init; a workspace for n rows serves calls of fewer).  One workspace serves one stream; graphs that may run at the same time need
+ * one each.  Its word 0 is the error word of the calls (sparq_async_error). */
+int sparq_paged_workspace_bytes(const sparq_paged_shape* shape, int32_t n, size_t* out_bytes);
+
+/* Write the call's rows into their pages, quantised in 8-bit pages.
+ *   k_new, v_new  device, cache dtype, 16-byte aligned, the same strides for both
+ * A sequence with more rows than positions (n_b > seq_lens[b]) or a length outside [0, S_bound] is left untouched
+ * (SPARQ_ERR_BAD_SEQ_LEN); a row whose page id lies outside the pool is not written (SPARQ_ERR_BAD_PAGE).  Sequences may share
+ * pages that the call does not write. */
+int sparq_paged_append(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows,
+                       const void* k_new, const void* v_new, const sparq_strides* strides,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Read rows back as 16-bit rows (value = code * scale, rounded to nearest-even): row t is the one at position first[b] + t.
+ *   first         device [B] or NULL (0 everywhere)
+ *   K_out, V_out  device, dtype, the same strides for both
+ * Rows at positions outside [0, seq_lens[b]) (SPARQ_ERR_BAD_SEQ_LEN) and on page ids outside the pool (SPARQ_ERR_BAD_PAGE) are left
+ * as they were. */
+int sparq_paged_read(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows,
+                     const int32_t* first, void* K_out, void* V_out, const sparq_strides* strides,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Attention of the call's rows over the pages: per row (position p) and query head
+ *   y = softmax_j(q . K_j / sqrt(d_h)) V_j over the positions j < seq_lens[b] that it sees: j <= p (unless SPARQ_FLAG_PAGED_ALL) and
+ *   j > p - window (if window > 0).
+ * Positions that a row does not see have no part in its result, whatever they hold.  A row that sees nothing (a sequence of
+ * length 0; one that starts before position 0), or only logits of -inf, is zeros with a logarithm of -inf; infinities and NaN among what it sees take their
+ * course.  Sums and the softmax's state are fp32, weights are rounded to 16 bits before the product with the values (fp16 for 8-bit
+ * pages), y is rounded to nearest-even.
+ *   q, out   device [.., H, .., d_h], dtype, 16-byte aligned; each with strides of its own; out must not overlap q
+ *   lse_out  device fp32 or NULL: the natural logarithm of the softmax's denominator, [B, H, n], or with row_start [H, n_rows]
+ * A length outside [0, S_bound] counts as 0 (SPARQ_ERR_BAD_SEQ_LEN); a page id outside the pool is taken as page 0
+ * (SPARQ_ERR_BAD_PAGE: the outputs of that sequence mean nothing).
+ */
+int sparq_paged_attention(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows,
+                          const void* q, const sparq_strides* q_strides, void* out, const sparq_strides* out_strides,
+                          float* lse_out, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 const char* sparq_status_string(int status);
 

@@ -19,11 +19,15 @@ SPARQ_F16, SPARQ_BF16 = 0, 1
 SPARQ_FLAG_NO_REALLOC, SPARQ_FLAG_GQA_SHARED, SPARQ_FLAG_RAGGED_BATCH = 1, 2, 4
 SPARQ_FLAG_TAU_SQRT_DH, SPARQ_FLAG_TAU_SQRT_R, SPARQ_FLAG_SINGLE_K, SPARQ_FLAG_TILED_K = 8, 16, 32, 64
 SPARQ_ERR_APPEND_FULL, SPARQ_ERR_EMPTY_SEQ, SPARQ_ERR_IDX_TRUNCATED, SPARQ_ERR_BAD_SEQ_LEN, SPARQ_ERR_INTERNAL = 1, 2, 4, 8, 16
+SPARQ_ERR_BAD_ROWS, SPARQ_ERR_BAD_PAGE = 32, 64
+SPARQ_PAGES_16, SPARQ_PAGES_I8, SPARQ_PAGES_E4M3 = 0, 1, 2
+SPARQ_FLAG_PAGED_ALL = 1
 SPARQ_OK, SPARQ_EINVAL, SPARQ_EUNSUPPORTED, SPARQ_EWORKSPACE, SPARQ_ELAUNCH, SPARQ_ETOOLARGE = 0, -1, -2, -3, -4, -5
 
 EXPORTS = ["sparq_workspace_bytes", "sparq_workspace_init", "sparq_kv_append", "sparq_decode", "sparq_decode_noalloc", "sparq_decode_step",
            "dense_decode", "sparq_async_error", "sparq_copy_probe", "sparq_read_probe", "sparq_decode_plan",
-           "sparq_stage_clocks", "sparq_status_string"]
+           "sparq_stage_clocks", "sparq_paged_workspace_bytes", "sparq_paged_append", "sparq_paged_read", "sparq_paged_attention",
+           "sparq_status_string"]
 
 
 class SparqShape(ctypes.Structure):
@@ -36,6 +40,26 @@ class SparqShape(ctypes.Structure):
 class SparqCache(ctypes.Structure):
     _fields_ = [("K", ctypes.c_void_p), ("Kt", ctypes.c_void_p), ("V", ctypes.c_void_p),
                 ("v_mean", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p)]
+
+
+class SparqPagedShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d_h", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("page_type", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("window", ctypes.c_int32), ("S_bound", ctypes.c_int32)]
+
+
+class SparqPagedCache(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p)]
+
+
+class SparqRows(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("n_per_seq", ctypes.c_void_p), ("row_start", ctypes.c_void_p)]
+
+
+class SparqStrides(ctypes.Structure):
+    _fields_ = [("seq", ctypes.c_int64), ("head", ctypes.c_int64), ("row", ctypes.c_int64)]
 
 
 class SparqError(RuntimeError):
@@ -68,6 +92,12 @@ def load() -> ctypes.CDLL:
     L.sparq_async_error.argtypes = [vp, ctypes.POINTER(i32), vp]
     L.sparq_copy_probe.argtypes = [vp, vp, sz, vp]
     L.sparq_read_probe.argtypes = [vp, sz, vp, sz, vp]
+    psh, pch = ctypes.POINTER(SparqPagedShape), ctypes.POINTER(SparqPagedCache)
+    rws, std = ctypes.POINTER(SparqRows), ctypes.POINTER(SparqStrides)
+    L.sparq_paged_workspace_bytes.argtypes = [psh, i32, ctypes.POINTER(sz)]
+    L.sparq_paged_append.argtypes = [psh, pch, rws, vp, vp, std, vp, sz, vp]
+    L.sparq_paged_read.argtypes = [psh, pch, rws, vp, vp, vp, std, vp, sz, vp]
+    L.sparq_paged_attention.argtypes = [psh, pch, rws, vp, std, vp, std, vp, vp, sz, vp]
     L.sparq_status_string.argtypes = [ctypes.c_int]
     L.sparq_decode_plan.argtypes = [shp]
     L.sparq_stage_clocks.argtypes = [shp, ctypes.POINTER(sz), ctypes.POINTER(i32), ctypes.POINTER(i32)]
@@ -203,3 +233,67 @@ def sparq_copy_probe(dst, src, n_bytes: int, stream=None) -> None:
 def sparq_read_probe(src, n_bytes: int, sink, stream=None) -> None:
     _check("sparq_read_probe", load().sparq_read_probe(_dev(src, "src"), int(n_bytes), _dev(sink, "sink"),
                                                        sink.numel() * sink.element_size(), _stream(stream)))
+
+
+# ---- the paged cache ----
+
+def make_paged_shape(B, H, H_kv, d_h, page_size, n_pages, max_pages, dtype, page_type=SPARQ_PAGES_16, flags=0, window=0, S_bound=0) -> SparqPagedShape:
+    code = {torch.float16: SPARQ_F16, torch.bfloat16: SPARQ_BF16}.get(dtype, dtype)
+    return SparqPagedShape(B, H, H_kv, d_h, page_size, n_pages, max_pages, int(code), page_type, flags, window, S_bound)
+
+
+def make_paged_cache(K, V, K_scale, V_scale, page_table, seq_lens) -> SparqPagedCache:
+    return SparqPagedCache(_dev(K, "K"), _dev(V, "V"), _dev(K_scale, "K_scale", torch.float32), _dev(V_scale, "V_scale", torch.float32),
+                           _dev(page_table, "page_table", torch.int32), _dev(seq_lens, "seq_lens", torch.int32))
+
+
+def make_rows(n: int, n_per_seq: Optional[torch.Tensor] = None, row_start: Optional[torch.Tensor] = None, n_rows: int = 0) -> SparqRows:
+    return SparqRows(int(n), int(n_rows), _dev(n_per_seq, "n_per_seq", torch.int32), _dev(row_start, "row_start", torch.int32))
+
+
+def _rows_dev(t: torch.Tensor, name: str, packed: bool):
+    """(pointer, strides) of rows [B, heads, n, d_h], or packed [n_rows, heads, d_h], in any order with contiguous channels."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in GPU memory (got {t.device}); the library has no CPU path")
+    s = t.stride()
+    if s[-1] != 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    return t.data_ptr(), SparqStrides(0, s[1], s[0]) if packed else SparqStrides(s[0], s[1], s[2])
+
+
+def sparq_paged_workspace_bytes(shape: SparqPagedShape, n: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("sparq_paged_workspace_bytes", load().sparq_paged_workspace_bytes(ctypes.byref(shape), int(n), ctypes.byref(out)))
+    return int(out.value)
+
+
+def _same_strides(a: torch.Tensor, b: torch.Tensor, what: str) -> None:
+    if a.stride() != b.stride() or a.shape != b.shape:
+        raise ValueError(f"{what} must have the same shape and strides")
+
+
+def sparq_paged_append(shape, cache, rows, k_new, v_new, workspace, stream=None) -> None:
+    packed = rows.row_start is not None
+    _same_strides(k_new, v_new, "k_new and v_new")
+    (k, s), (v, _) = _rows_dev(k_new, "k_new", packed), _rows_dev(v_new, "v_new", packed)
+    _check("sparq_paged_append",
+           load().sparq_paged_append(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), k, v, ctypes.byref(s),
+                                     _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def sparq_paged_read(shape, cache, rows, first, K_out, V_out, workspace, stream=None) -> None:
+    packed = rows.row_start is not None
+    _same_strides(K_out, V_out, "K_out and V_out")
+    (k, s), (v, _) = _rows_dev(K_out, "K_out", packed), _rows_dev(V_out, "V_out", packed)
+    _check("sparq_paged_read",
+           load().sparq_paged_read(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), _dev(first, "first", torch.int32), k, v,
+                                   ctypes.byref(s), _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def sparq_paged_attention(shape, cache, rows, q, out, lse_out, workspace, stream=None) -> None:
+    packed = rows.row_start is not None
+    (qp, qs), (op, os_) = _rows_dev(q, "q", packed), _rows_dev(out, "out", packed)
+    _check("sparq_paged_attention",
+           load().sparq_paged_attention(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), qp, ctypes.byref(qs), op, ctypes.byref(os_),
+                                        _dev(lse_out, "lse_out", torch.float32), _dev(workspace, "workspace"),
+                                        workspace.numel() * workspace.element_size(), _stream(stream)))

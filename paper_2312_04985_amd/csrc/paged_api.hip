@@ -1,0 +1,135 @@
+// C ABI of the paged cache (include/sparq.h): argument validation, launch planning, enqueue.
+#include "../../include/sparq.h"
+
+#include <hip/hip_runtime.h>
+
+#include "paged.h"
+
+static_assert((int)sparq::kPages16 == SPARQ_PAGES_16 && (int)sparq::kPagesI8 == SPARQ_PAGES_I8 && (int)sparq::kPagesE4M3 == SPARQ_PAGES_E4M3, "page types");
+static_assert(sparq::kErrBadSeqLen == SPARQ_ERR_BAD_SEQ_LEN && sparq::kErrBadRows == SPARQ_ERR_BAD_ROWS && sparq::kErrBadPage == SPARQ_ERR_BAD_PAGE, "error bits");
+
+namespace {
+
+using namespace sparq;
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int check_paged_shape(const sparq_paged_shape* s) {
+  if (!s) return SPARQ_EINVAL;
+  if (s->B < 1 || s->H < 1 || s->H_kv < 1 || s->d_h < 1 || s->H % s->H_kv != 0) return SPARQ_EINVAL;
+  if (s->page_size < 16 || s->page_size % 16 != 0 || s->n_pages < 1 || s->max_pages < 1) return SPARQ_EINVAL;
+  const int64_t capacity = (int64_t)s->max_pages * s->page_size;
+  if (capacity > INT32_MAX) return SPARQ_EINVAL;
+  if (s->dtype != SPARQ_F16 && s->dtype != SPARQ_BF16) return SPARQ_EINVAL;
+  if (s->page_type != SPARQ_PAGES_16 && s->page_type != SPARQ_PAGES_I8 && s->page_type != SPARQ_PAGES_E4M3) return SPARQ_EINVAL;
+  if (s->flags & ~(uint32_t)SPARQ_FLAG_PAGED_ALL) return SPARQ_EINVAL;
+  if (s->window < 0 || s->S_bound < 0 || s->S_bound > capacity) return SPARQ_EINVAL;
+  if (s->d_h != 64 && s->d_h != 128 && s->d_h != 256) return SPARQ_EUNSUPPORTED;
+  if ((int64_t)s->B * s->H > (int64_t)1 << 30) return SPARQ_EUNSUPPORTED;
+  return SPARQ_OK;
+}
+
+int check_rows(const sparq_paged_shape* s, const sparq_rows* r) {
+  if (!r || r->n < 1 || (r->n_per_seq && r->row_start)) return SPARQ_EINVAL;
+  if (r->row_start && r->n_rows < 1) return SPARQ_EINVAL;
+  // (row numbers of a launch, B n H, are formed in 32 bits)
+  if ((int64_t)s->B * r->n > INT32_MAX / s->H) return SPARQ_EUNSUPPORTED;
+  return SPARQ_OK;
+}
+
+// `written`: rows must not lie on top of each other
+int check_strides(const sparq_paged_shape* s, const sparq_rows* r, const sparq_strides* t, int heads, bool written) {
+  if (!t || t->seq < 0 || t->head < 0 || t->row < 0) return SPARQ_EINVAL;
+  if (t->seq % 8 || t->head % 8 || t->row % 8) return SPARQ_EINVAL;
+  if (!written) return SPARQ_OK;
+  if (!r->row_start && s->B > 1 && t->seq < s->d_h) return SPARQ_EINVAL;
+  if (heads > 1 && t->head < s->d_h) return SPARQ_EINVAL;
+  if ((r->row_start ? r->n_rows : r->n) > 1 && t->row < s->d_h) return SPARQ_EINVAL;
+  return SPARQ_OK;
+}
+
+int check_paged_cache(const sparq_paged_shape* s, const sparq_paged_cache* c) {
+  if (!c || !c->K || !c->V || !c->page_table || !c->seq_lens) return SPARQ_EINVAL;
+  if (!aligned16(c->K) || !aligned16(c->V)) return SPARQ_EINVAL;
+  if (s->page_type != SPARQ_PAGES_16 && (!c->K_scale || !c->V_scale || !aligned16(c->K_scale) || !aligned16(c->V_scale))) return SPARQ_EINVAL;
+  return SPARQ_OK;
+}
+
+size_t paged_workspace(const sparq_paged_shape*, int) { return kControlBytes; }
+
+// everything that the calls have in common
+int check_call(const sparq_paged_shape* s, const sparq_paged_cache* c, const sparq_rows* r, const void* ws, size_t ws_bytes) {
+  int rc = check_paged_shape(s);
+  if (rc == SPARQ_OK) rc = check_paged_cache(s, c);
+  if (rc == SPARQ_OK) rc = check_rows(s, r);
+  if (rc != SPARQ_OK) return rc;
+  if (!ws || !aligned16(ws) || ws_bytes < paged_workspace(s, r->n)) return SPARQ_EWORKSPACE;
+  return SPARQ_OK;
+}
+
+PagedArgs paged_args(const sparq_paged_shape* s, const sparq_paged_cache* c, const sparq_rows* r, void* ws) {
+  PagedArgs p{};
+  p.K = c->K; p.V = c->V; p.K_scale = c->K_scale; p.V_scale = c->V_scale; p.page_table = c->page_table; p.seq_lens = c->seq_lens;
+  p.n_per_seq = r->n_per_seq; p.row_start = r->row_start; p.err = static_cast<int32_t*>(ws);
+  p.B = s->B; p.H = s->H; p.H_kv = s->H_kv; p.d_h = s->d_h; p.page_size = s->page_size; p.n_pages = s->n_pages; p.max_pages = s->max_pages;
+  p.bound = s->S_bound > 0 ? s->S_bound : s->max_pages * s->page_size;
+  p.n = r->n; p.n_rows = r->row_start ? r->n_rows : 0;
+  p.by_page = make_divider(s->page_size); p.by_H_kv = make_divider(s->H_kv); p.by_n = make_divider(r->n);
+  return p;
+}
+
+RowStrides strides_of(const sparq_strides* t) { return RowStrides{t->seq, t->head, t->row}; }
+
+int move_rows(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows, const int32_t* first, void* k, void* v,
+              const sparq_strides* strides, void* workspace, size_t workspace_bytes, void* hip_stream, bool reads) {
+  int rc = check_call(shape, cache, rows, workspace, workspace_bytes);
+  if (rc == SPARQ_OK && (!k || !v || !aligned16(k) || !aligned16(v))) rc = SPARQ_EINVAL;
+  if (rc == SPARQ_OK) rc = check_strides(shape, rows, strides, shape->H_kv, reads);
+  if (rc != SPARQ_OK) return rc;
+  PagedRowsArgs a{};
+  a.p = paged_args(shape, cache, rows, workspace);
+  a.k = k; a.v = v; a.first = first; a.s = strides_of(strides);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t e = reads ? launch_paged_read(a, shape->dtype, shape->page_type, s) : launch_paged_append(a, shape->dtype, shape->page_type, s);
+  return e == hipSuccess ? SPARQ_OK : SPARQ_ELAUNCH;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sparq_paged_workspace_bytes(const sparq_paged_shape* shape, int32_t n, size_t* out_bytes) {
+  const int rc = check_paged_shape(shape);
+  if (rc != SPARQ_OK) return rc;
+  if (n < 1 || !out_bytes) return SPARQ_EINVAL;
+  *out_bytes = paged_workspace(shape, n);
+  return SPARQ_OK;
+}
+
+int sparq_paged_append(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows, const void* k_new, const void* v_new,
+                       const sparq_strides* strides, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return move_rows(shape, cache, rows, nullptr, const_cast<void*>(k_new), const_cast<void*>(v_new), strides, workspace, workspace_bytes, hip_stream, false);
+}
+
+int sparq_paged_read(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows, const int32_t* first, void* K_out, void* V_out,
+                     const sparq_strides* strides, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return move_rows(shape, cache, rows, first, K_out, V_out, strides, workspace, workspace_bytes, hip_stream, true);
+}
+
+int sparq_paged_attention(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows, const void* q, const sparq_strides* q_strides,
+                          void* out, const sparq_strides* out_strides, float* lse_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_call(shape, cache, rows, workspace, workspace_bytes);
+  if (rc == SPARQ_OK && (!q || !out || !aligned16(q) || !aligned16(out))) rc = SPARQ_EINVAL;
+  if (rc == SPARQ_OK) rc = check_strides(shape, rows, q_strides, shape->H, false);
+  if (rc == SPARQ_OK) rc = check_strides(shape, rows, out_strides, shape->H, true);
+  if (rc != SPARQ_OK) return rc;
+  PagedAttendArgs a{};
+  a.p = paged_args(shape, cache, rows, workspace);
+  a.q = q; a.out = out; a.lse = lse_out; a.qs = strides_of(q_strides); a.os = strides_of(out_strides);
+  a.window = shape->window; a.all = (shape->flags & SPARQ_FLAG_PAGED_ALL) != 0;
+  a.group = shape->H / shape->H_kv; a.by_group = make_divider(a.group);
+  const hipError_t e = launch_paged_attend(a, shape->dtype, shape->page_type, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? SPARQ_OK : SPARQ_ELAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,155 @@
+"""Device buffers of one paged cache and convenience wrappers over the binding.
+
+Allocation and bookkeeping only (torch owns the memory); all work is done by libsparq.
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple, Union
+
+import torch
+
+from . import binding as B
+
+PAGE_TYPES = {"16": B.SPARQ_PAGES_16, "i8": B.SPARQ_PAGES_I8, "e4m3": B.SPARQ_PAGES_E4M3}
+CODE_TYPES = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+class PagedCache:
+    """A pool of pages for K and V, a page table and lengths: K, V [n_pages, H_kv, page_size, d_h], page_table [B, max_pages],
+    seq_lens [B] (int32, the caller's: which page a sequence gets and how long it is are decided by whoever schedules the batch).
+
+    seq_lens counts the rows of the call that is made: raise it first, then append the new rows and attend with their queries.
+    Rows are [B, heads, n, d_h] in any order with contiguous channels ([B, heads, d_h] for one row each), of which sequence b has
+    n_new_per_seq[b] (all n without it); or packed [n_rows, heads, d_h] with row_start [B + 1] and n_new, the most rows of a sequence.
+    """
+
+    def __init__(self, Bsz: int, H: int, H_kv: int, d_h: int, page_size: int, n_pages: int, max_pages: int, dtype, pages: str = "16",
+                 device="cuda", causal: bool = True, window: int = 0):
+        if pages not in PAGE_TYPES:
+            raise ValueError(f"pages must be one of {sorted(PAGE_TYPES)}, got {pages!r}")
+        mk = lambda *size, dtype: torch.zeros(size, dtype=dtype, device=device)   # noqa: E731
+        pool = CODE_TYPES.get(pages, dtype)
+        scale = (lambda: mk(n_pages, H_kv, page_size, dtype=torch.float32)) if pages != "16" else (lambda: None)
+        self._hold(mk(n_pages, H_kv, page_size, d_h, dtype=pool), mk(n_pages, H_kv, page_size, d_h, dtype=pool), mk(Bsz, max_pages, dtype=torch.int32),
+                   mk(Bsz, dtype=torch.int32), H, dtype, scale(), scale(), causal, window)
+
+    @classmethod
+    def over(cls, K: torch.Tensor, V: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor, H: int, dtype,
+             K_scale: Optional[torch.Tensor] = None, V_scale: Optional[torch.Tensor] = None, causal: bool = True, window: int = 0) -> "PagedCache":
+        """The same over buffers that exist already; the pools' dtype says what the pages hold."""
+        c = cls.__new__(cls)
+        c._hold(K, V, page_table, seq_lens, H, dtype, K_scale, V_scale, causal, window)
+        return c
+
+    def _hold(self, K, V, page_table, seq_lens, H, dtype, K_scale, V_scale, causal, window):
+        kinds = {dtype: "16", torch.int8: "i8", torch.float8_e4m3fn: "e4m3"}
+        if K.dim() != 4 or K.shape != V.shape or K.dtype != V.dtype or K.dtype not in kinds:
+            raise ValueError("K and V must be pools [n_pages, H_kv, page_size, d_h] of the rows' dtype, int8 or float8_e4m3fn")
+        n_pages, H_kv, page_size, d_h = K.shape
+        Bsz, max_pages = page_table.shape
+        if seq_lens.shape != (Bsz,):
+            raise ValueError("seq_lens must be [B], page_table [B, max_pages]")
+        self.pages = kinds[K.dtype]
+        for name, s in (("K_scale", K_scale), ("V_scale", V_scale)):
+            if self.pages != "16" and (s is None or s.shape != (n_pages, H_kv, page_size)):
+                raise ValueError(f"{name} must be [n_pages, H_kv, page_size] for 8-bit pages")
+        if self.pages == "16":
+            K_scale = V_scale = None
+        for t in (K, V, page_table, seq_lens, K_scale, V_scale):
+            if t is not None and t.device != K.device:
+                raise ValueError("all buffers of a cache must live on one device")
+        self.K, self.V, self.K_scale, self.V_scale, self.page_table, self.seq_lens = K, V, K_scale, V_scale, page_table, seq_lens
+        self.B, self.H, self.H_kv, self.d_h, self.page_size, self.n_pages, self.max_pages = Bsz, H, H_kv, d_h, page_size, n_pages, max_pages
+        self.dtype, self.device = dtype, K.device
+        self.cache = B.make_paged_cache(K, V, K_scale, V_scale, page_table, seq_lens)
+        self.shape = B.make_paged_shape(Bsz, H, H_kv, d_h, page_size, n_pages, max_pages, dtype, PAGE_TYPES[self.pages],
+                                        0 if causal else B.SPARQ_FLAG_PAGED_ALL, window)
+        self.workspace = torch.zeros((B.sparq_paged_workspace_bytes(self.shape, 1),), dtype=torch.uint8, device=self.device)
+        self._rows_room = 1
+        with torch.cuda.device(self.device):
+            B.sparq_workspace_init(self.workspace)
+
+    def with_bound(self, S_bound: int) -> "PagedCache":
+        """Promise that no sequence is longer than S_bound (0: what the page table has room for)."""
+        self.shape.S_bound = S_bound
+        self._rows_room = 0
+        return self
+
+    # ---- the calls ----
+    def _call(self, t: torch.Tensor, heads: int, n_new, n_new_per_seq, row_start) -> Tuple[torch.Tensor, "B.SparqRows"]:
+        """The rows of a call and what says which they are; a workspace that is large enough."""
+        if t.dtype != self.dtype or t.device != self.device:
+            raise ValueError(f"rows must be {self.dtype} on {self.device}, got {t.dtype} on {t.device}")
+        if row_start is None:
+            t = t.unsqueeze(2) if t.dim() == 3 else t
+            if t.dim() != 4 or t.shape[0] != self.B or t.shape[1] != heads or t.shape[3] != self.d_h:
+                raise ValueError(f"rows must be [{self.B}, {heads}, n, {self.d_h}], got {tuple(t.shape)}")
+            if n_new is not None and n_new != t.shape[2]:
+                raise ValueError("n_new is the rows' third size where they are not packed")
+            n, n_rows = t.shape[2], 0
+        else:
+            if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.d_h:
+                raise ValueError(f"packed rows must be [n_rows, {heads}, {self.d_h}], got {tuple(t.shape)}")
+            if n_new is None:
+                raise ValueError("packed rows need n_new, the most rows of a sequence")
+            if row_start.shape != (self.B + 1,):
+                raise ValueError("row_start must be [B + 1]")
+            n, n_rows = n_new, t.shape[0]
+        if n_new_per_seq is not None and n_new_per_seq.shape != (self.B,):
+            raise ValueError("n_new_per_seq must be [B]")
+        for x in (n_new_per_seq, row_start):
+            if x is not None and x.device != self.device:
+                raise ValueError(f"row counts must live on {self.device}")
+        if n > self._rows_room:
+            need = B.sparq_paged_workspace_bytes(self.shape, n)
+            if need > self.workspace.numel():
+                self.workspace = torch.zeros((need,), dtype=torch.uint8, device=self.device)
+                B.sparq_workspace_init(self.workspace, torch.cuda.current_stream(self.device))
+            self._rows_room = n
+        return t, B.make_rows(n, n_new_per_seq, row_start, n_rows)
+
+    def _on(self, stream):
+        return torch.cuda.current_stream(self.device) if stream is None else stream
+
+    def append(self, k_new: torch.Tensor, v_new: torch.Tensor, n_new_per_seq: Optional[torch.Tensor] = None,
+               row_start: Optional[torch.Tensor] = None, n_new: Optional[int] = None, stream=None) -> None:
+        """Write the rows at the last positions of every sequence (heads: H_kv)."""
+        with torch.cuda.device(self.device):
+            k_new, rows = self._call(k_new, self.H_kv, n_new, n_new_per_seq, row_start)
+            v_new, _ = self._call(v_new, self.H_kv, n_new, n_new_per_seq, row_start)
+            B.sparq_paged_append(self.shape, self.cache, rows, k_new, v_new, self.workspace, self._on(stream))
+
+    def attend(self, q: torch.Tensor, n_new_per_seq: Optional[torch.Tensor] = None, row_start: Optional[torch.Tensor] = None,
+               n_new: Optional[int] = None, out: Optional[torch.Tensor] = None, lse: Union[None, bool, torch.Tensor] = None, stream=None):
+        """Attention of the last rows of every sequence (heads: H).  lse: True, or a float32 tensor for the logarithms of the
+        denominators, [B, H, n] or packed [H, n_rows]; (out, lse) is returned if it is True."""
+        with torch.cuda.device(self.device):
+            q4, rows = self._call(q, self.H, n_new, n_new_per_seq, row_start)
+            if out is None:      # rows that belong to no sequence are not written
+                out = torch.empty_like(q) if n_new_per_seq is None and row_start is None else torch.zeros_like(q)
+            elif out.shape != q.shape:
+                raise ValueError("out must have q's shape")
+            o4, _ = self._call(out, self.H, n_new, n_new_per_seq, row_start)
+            size = (self.H, q.shape[0]) if row_start is not None else (self.B, self.H, q4.shape[2])
+            lse_out = None
+            if lse is not None and lse is not False:
+                lse_out = torch.full(size, -float("inf"), dtype=torch.float32, device=self.device) if lse is True else lse
+                if lse_out.shape != size or lse_out.device != self.device:
+                    raise ValueError(f"lse must be {size} on {self.device}")
+            B.sparq_paged_attention(self.shape, self.cache, rows, q4, o4, lse_out, self.workspace, self._on(stream))
+            return (out, lse_out) if lse is True else out
+
+    def read(self, K_out: torch.Tensor, V_out: torch.Tensor, first: Optional[torch.Tensor] = None, n_per_seq: Optional[torch.Tensor] = None,
+             row_start: Optional[torch.Tensor] = None, n_new: Optional[int] = None, stream=None):
+        """Rows first[b] .. (0 .. without it) of every sequence as 16-bit rows, into K_out and V_out (heads: H_kv); they are returned."""
+        with torch.cuda.device(self.device):
+            k, rows = self._call(K_out, self.H_kv, n_new, n_per_seq, row_start)
+            v, _ = self._call(V_out, self.H_kv, n_new, n_per_seq, row_start)
+            if first is not None and first.shape != (self.B,):
+                raise ValueError("first must be [B]")
+            B.sparq_paged_read(self.shape, self.cache, rows, first, k, v, self.workspace, self._on(stream))
+            return K_out, V_out
+
+    def error_flags(self) -> int:
+        with torch.cuda.device(self.device):
+            return B.sparq_async_error(self.workspace, torch.cuda.current_stream(self.device))
