@@ -304,7 +304,7 @@ typedef struct {
   int32_t B, H, H_kv, d_h;   /* d_h 64, 128 or 256 */
   int32_t page_size;         /* positions per page, a multiple of 16 */
   int32_t n_pages;           /* pages of the pool */
-  int32_t max_pages;         /* entries per row of the page table; max_pages * page_size < 2^31 */
+  int32_t max_pages;         /* entries per row of the page table; max_pages * page_size < 2^31 - 2^16 */
   int32_t dtype;             /* sparq_dtype of rows, queries and outputs, and of 16-bit pages */
   int32_t page_type;         /* sparq_page_type */
   uint32_t flags;

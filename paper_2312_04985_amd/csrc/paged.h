@@ -39,6 +39,7 @@ struct PagedAttendArgs {
   int32_t window, all;                                  // all: not causal
   int32_t group;                                        // query heads per KV head
   int32_t n_tiles;                                      // row tiles per (sequence, KV head)
+  int32_t skip_rows;                                    // sequences of up to this many rows (times group) are another launch's
   Divider by_group;
 };
 
@@ -79,8 +80,21 @@ __host__ __device__ inline int64_t pool_row(const PagedArgs& a, int page, int he
   return ((int64_t)page * a.H_kv + head) * a.page_size + slot;
 }
 
+// Few rows per (sequence, KV head): the launch's workgroups and what they leave for each other.
+struct TokensPlan {
+  int workgroups, max_rows;                             // max_rows: tokens times group, 0: no sequence is served that way
+  float* partials;                                      // [workgroups][2][16, 32 or 64][d_h + 4]
+  int32_t* tickets;                                     // [workgroups], 0 between launches
+};
+// The most rows that a workgroup's registers hold next to the positions in flight.
+constexpr int tokens_rows(int d_h) { return d_h == 64 ? 64 : (d_h == 128 ? 32 : 16); }
+// Workgroups per CU: the 32 KB that a wave has in flight at 256 channels of 16 bits leave room for one.
+constexpr int tokens_per_cu(int d_h, int page_type) { return d_h == 256 && page_type == kPages16 ? 1 : 2; }
+constexpr int kTokensWorkgroups = 512;                  // at most
+
 hipError_t launch_paged_append(const PagedRowsArgs& a, int dtype, int page_type, hipStream_t s);
 hipError_t launch_paged_read(const PagedRowsArgs& a, int dtype, int page_type, hipStream_t s);
-hipError_t launch_paged_attend(const PagedAttendArgs& a, int dtype, int page_type, hipStream_t s);
+hipError_t launch_paged_chunk(const PagedAttendArgs& a, int dtype, int page_type, hipStream_t s);
+hipError_t launch_paged_tokens(const PagedAttendArgs& a, const TokensPlan& t, int dtype, int page_type, hipStream_t s);
 
 }  // namespace sparq

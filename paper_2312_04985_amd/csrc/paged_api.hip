@@ -19,7 +19,7 @@ int check_paged_shape(const sparq_paged_shape* s) {
   if (s->B < 1 || s->H < 1 || s->H_kv < 1 || s->d_h < 1 || s->H % s->H_kv != 0) return SPARQ_EINVAL;
   if (s->page_size < 16 || s->page_size % 16 != 0 || s->n_pages < 1 || s->max_pages < 1) return SPARQ_EINVAL;
   const int64_t capacity = (int64_t)s->max_pages * s->page_size;
-  if (capacity > INT32_MAX) return SPARQ_EINVAL;
+  if (capacity > INT32_MAX - (1 << 16)) return SPARQ_EINVAL;      // (positions are counted up in steps behind the last one)
   if (s->dtype != SPARQ_F16 && s->dtype != SPARQ_BF16) return SPARQ_EINVAL;
   if (s->page_type != SPARQ_PAGES_16 && s->page_type != SPARQ_PAGES_I8 && s->page_type != SPARQ_PAGES_E4M3) return SPARQ_EINVAL;
   if (s->flags & ~(uint32_t)SPARQ_FLAG_PAGED_ALL) return SPARQ_EINVAL;
@@ -55,7 +55,33 @@ int check_paged_cache(const sparq_paged_shape* s, const sparq_paged_cache* c) {
   return SPARQ_OK;
 }
 
-size_t paged_workspace(const sparq_paged_shape*, int) { return kControlBytes; }
+// How an attention call is served: by the kernel whose waves divide the positions where all rows of a KV head (tokens times
+// group) fit one workgroup's registers, by the kernel whose waves divide the rows otherwise; by both where only the
+// device knows how many rows each sequence has: single tokens then go to the first, longer chunks to the second.
+struct AttendPlan { int tokens_rows, chunk; };   // rows that the first kernel takes at most (0: not launched); whether the second is launched
+
+AttendPlan attend_plan(const sparq_paged_shape* s, int n, bool counted) {
+  const int64_t g = s->H / s->H_kv, most = tokens_rows(s->d_h);
+  if (n * g <= most) return {(int)(n * g), 0};
+  if (!counted) return {0, 1};
+  const int64_t single = (g + 15) / 16 * 16;
+  return {single <= most ? (int)single : 0, 1};
+}
+
+int tokens_tile(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
+
+// Workgroups of the first kernel: what runs at once, and no more than 64 for a unit, whose last one puts their results together.
+int tokens_workgroups(const sparq_paged_shape* s) {
+  const int64_t units = (int64_t)s->B * s->H_kv, most = 256 * tokens_per_cu(s->d_h, s->page_type);
+  return (int)(units * 64 < most ? units * 64 : most);
+}
+
+// (calls of fewer rows than n need no more: they have at most as many rows per KV head as are counted here)
+size_t paged_workspace(const sparq_paged_shape* s, int n) {
+  const int64_t rows = (int64_t)n * (s->H / s->H_kv), most = tokens_rows(s->d_h);
+  const int tile = tokens_tile((int)(rows < most ? rows : most));
+  return (size_t)kControlBytes + (size_t)tokens_workgroups(s) * 2 * tile * (s->d_h + 4) * sizeof(float);
+}
 
 // everything that the calls have in common
 int check_call(const sparq_paged_shape* s, const sparq_paged_cache* c, const sparq_rows* r, const void* ws, size_t ws_bytes) {
@@ -66,6 +92,8 @@ int check_call(const sparq_paged_shape* s, const sparq_paged_cache* c, const spa
   if (!ws || !aligned16(ws) || ws_bytes < paged_workspace(s, r->n)) return SPARQ_EWORKSPACE;
   return SPARQ_OK;
 }
+
+static_assert(kTokensWorkgroups <= kTickets, "a counter per workgroup");
 
 PagedArgs paged_args(const sparq_paged_shape* s, const sparq_paged_cache* c, const sparq_rows* r, void* ws) {
   PagedArgs p{};
@@ -128,7 +156,16 @@ int sparq_paged_attention(const sparq_paged_shape* shape, const sparq_paged_cach
   a.q = q; a.out = out; a.lse = lse_out; a.qs = strides_of(q_strides); a.os = strides_of(out_strides);
   a.window = shape->window; a.all = (shape->flags & SPARQ_FLAG_PAGED_ALL) != 0;
   a.group = shape->H / shape->H_kv; a.by_group = make_divider(a.group);
-  const hipError_t e = launch_paged_attend(a, shape->dtype, shape->page_type, static_cast<hipStream_t>(hip_stream));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const AttendPlan plan = attend_plan(shape, rows->n, rows->n_per_seq || rows->row_start);
+  hipError_t e = hipSuccess;
+  if (plan.tokens_rows) {
+    const TokensPlan t{tokens_workgroups(shape), plan.tokens_rows, reinterpret_cast<float*>(static_cast<char*>(workspace) + kControlBytes),
+                       reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kTicketOffset)};
+    e = launch_paged_tokens(a, t, shape->dtype, shape->page_type, s);
+  }
+  a.skip_rows = plan.tokens_rows;
+  if (e == hipSuccess && plan.chunk) e = launch_paged_chunk(a, shape->dtype, shape->page_type, s);
   return e == hipSuccess ? SPARQ_OK : SPARQ_ELAUNCH;
 }
 

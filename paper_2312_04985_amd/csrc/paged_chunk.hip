@@ -1,4 +1,4 @@
-// Attention of new tokens over a paged cache: sparq_paged_attention.
+// Attention of many rows per (sequence, KV head) over a paged cache: chunks of new tokens, whole prompts.
 //
 // A workgroup serves 32 rows per wave of one (sequence, KV head): row m stands for token m / g and query head m % g of the
 // group, so that the heads of a group share what is read of the cache.  It walks the positions that its rows see in tiles
@@ -11,17 +11,10 @@
 // 8-bit pages: every code is a 16-bit float, so the products are those of 16-bit pages; a key's scale multiplies its scores.
 // A value's scale goes into the exponent: w_j = 2^(x_j + log2 s_j - m) <= 1 is what multiplies the codes, and w_j / s_j what
 // is summed.  Neither needs a rounding that 16-bit pages do not have.
-#include "paged_codes.h"
-
-#include <type_traits>
+#include "paged_core.h"
 
 namespace sparq {
 namespace {
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 64;               // positions per tile
 
@@ -35,13 +28,6 @@ template <> __device__ __forceinline__ f32x16 mfma_32x32x16<BF16>(const uint4& a
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Four 16-bit elements of a column: each group of 16 lanes reads 4 rows of 16 elements (lanes 4 r .. 4 r + 3 point at the
-// four 8-byte pieces of row r), lane i of the group gets column i.
-__device__ __forceinline__ uint2 lds_read_transposed(uint16_t* p) {
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
-}
-
 // Rows of DH elements in LDS in pieces of 8 (16 bytes).  Keys are read by 32 rows at one piece, values by 8 rows at 4
 // neighbouring pieces: both are spread over the banks by changing the pieces' places with the row.
 template <int DH> __device__ __forceinline__ int key_piece(int row, int piece) { return row * DH + ((piece ^ (row & (DH / 8 - 1) & 15)) << 3); }
@@ -50,21 +36,9 @@ template <int DH> __device__ __forceinline__ int value_piece(int row, int piece)
   return row * DH + ((piece ^ turn) << 3);
 }
 
-// whether one of eight 16-bit values is an infinity or NaN
-template <class T> __device__ __forceinline__ bool has_special(const uint4& v) {
-  constexpr uint32_t e = std::is_same_v<T, F16> ? 0x7c00u : 0x7f80u;
-  bool found = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t w = (&v.x)[i];
-    found = found || (w & e) == e || ((w >> 16) & e) == e;
-  }
-  return found;
-}
-
 template <class T, int PT, int DH, int NW>
 __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) {
-  using E = std::conditional_t<PT == kPages16, T, F16>;      // the products' type
+  using E = Product<T, PT>;
   constexpr int NT = NW * 64, ROWS = NW * 32, PIECES = DH / 8;
   __shared__ __align__(16) uint16_t Kt[kTile * DH], Vt[kTile * DH];
   __shared__ __align__(16) float s_k[kTile], s_log[kTile], s_inv[kTile];   // 8-bit pages: scale of the key, log2 and inverse of the value's
@@ -80,25 +54,17 @@ __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) 
   const SeqRows r = seq_rows(p.seq_lens[b], p.bound, p.n, p.n_per_seq, p.row_start, p.n_rows, b);
   if (r.err && tid == 0 && hk == 0 && tile == 0) atomicOr(p.err, r.err);
   const int M = r.n * a.group, m0 = tile * ROWS;
-  if (m0 >= M) return;
+  if (m0 >= M || M <= a.skip_rows) return;
   const bool packed = p.row_start != nullptr;
 
-  // what the lane's row sees: positions [lo, hi)
-  auto sees = [&](int t, int& lo, int& hi) {
-    const int pos = r.S - r.n + t;
-    hi = a.all ? r.S : pos + 1;
-    lo = a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
-  };
   const int m_w = m0 + wave * 32, m_last = M - 1;
   const bool live = m_w < M;                                   // a wave without rows only helps to load
   const int m = m_w + col < M ? m_w + col : m_last;
   const int t = divided(m, a.by_group), head = hk * a.group + m - t * a.group;
-  int lo, hi, wg_lo, wg_hi, wg_lo_last, wg_hi_first, w_lo_first, w_lo_last, w_hi_first, w_hi_last;
-  sees(t, lo, hi);
-  sees(divided(m0, a.by_group), wg_lo, wg_hi_first);
-  sees(divided(m0 + ROWS <= M ? m0 + ROWS - 1 : m_last, a.by_group), wg_lo_last, wg_hi);
-  sees(divided(live ? m_w : m_last, a.by_group), w_lo_first, w_hi_first);
-  sees(divided(m_w + 31 < M ? m_w + 31 : m_last, a.by_group), w_lo_last, w_hi_last);
+  const auto row_sees = [&](int m) { return seen_by(a, r, divided(m < M ? m : m_last, a.by_group)); };
+  const Seen mine = seen_by(a, r, t), wg_first = row_sees(m0), wg_last = row_sees(m0 + ROWS - 1), w_first = row_sees(m_w), w_last = row_sees(m_w + 31);
+  const int lo = mine.lo;
+  const uint32_t len = mine.hi > lo ? (uint32_t)(mine.hi - lo) : 0u;
 
   // the lane's part of its row of Q: channels 16 s + 8 half .. + 7
   uint4 qf[DH / 16];
@@ -106,31 +72,7 @@ __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) 
 #pragma unroll
   for (int s = 0; s < DH / 16; ++s) qf[s] = *reinterpret_cast<const uint4*>(qp + s * 16);
   float c_row = kLog2e / sqrtf((float)DH);                     // scores to exponents of 2
-  if constexpr (PT != kPages16 && std::is_same_v<T, BF16>) {
-    // The codes are products of fp16: the row is brought to a largest magnitude in [2^14, 2^15), by a power of 2, where fp16
-    // holds every bf16 value down to 2^-32 of it exactly and the rest to within 2^-40 of it.
-    uint32_t top = 0;
-#pragma unroll
-    for (int s = 0; s < DH / 16; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t w = (&qf[s].x)[i], x0 = w & 0x7f80u, x1 = (w >> 16) & 0x7f80u;
-        if (x0 < 0x7f80u && x0 > top) top = x0;
-        if (x1 < 0x7f80u && x1 > top) top = x1;
-      }
-    const uint32_t other = __shfl_xor(top, 32);
-    top = other > top ? other : top;
-    int e = (int)(top >> 7) - 127;                             // exponent of the largest finite magnitude
-    e = e < -112 ? -112 : e;                                   // (2^(14 - e) stays a float)
-    const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
-    c_row *= __uint_as_float((uint32_t)(e - 14 + 127) << 23);
-#pragma unroll
-    for (int s = 0; s < DH / 16; ++s) {
-      float f[8];
-      unpack8<BF16>(qf[s], f);
-      qf[s] = make_uint4(narrow2<F16>(f[0] * up, f[1] * up), narrow2<F16>(f[2] * up, f[3] * up), narrow2<F16>(f[4] * up, f[5] * up), narrow2<F16>(f[6] * up, f[7] * up));
-    }
-  }
+  if constexpr (PT != kPages16 && std::is_same_v<T, BF16>) query_to_half<32>(qf, c_row);
 
   f32x16 O[DH / 32];
 #pragma unroll
@@ -139,8 +81,8 @@ __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) 
     for (int i = 0; i < 16; ++i) O[j][i] = 0.0f;
   float m_ref = -INFINITY, l = 0.0f;
 
-  const int begin = wg_lo / kTile * kTile;
-  for (int p0 = begin; p0 < wg_hi; p0 += kTile) {
+  const int begin = wg_first.lo / kTile * kTile;
+  for (int p0 = begin; p0 < wg_last.hi; p0 += kTile) {
     // ---- the tile into LDS: 16 rows of a page per turn of a wave ----
     for (int g = wave; g < kTile / 16; g += NW) {
       const int pos0 = p0 + g * 16;
@@ -178,7 +120,7 @@ __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) 
         }
         if (lane < 16) {
           const float sk = p.K_scale[row + lane], sv = p.V_scale[row + lane];
-          const float v = sv < kLeastMagnitude / 1024.0f ? kLeastMagnitude / 1024.0f : sv;   // (a scale of 0: rows of zeros; NaN stays)
+          const float v = value_scale(sv);
           s_k[g * 16 + lane] = sk;
           s_log[g * 16 + lane] = log2_normal(v);
           s_inv[g * 16 + lane] = 1.0f / v;
@@ -189,7 +131,7 @@ __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) 
 
     // ---- scores, exponents, weights ----
     // (a row's exponent of 2 at position j is x_j = c q . K_j, with 8-bit pages plus log2 s_j)
-    const bool active = live && p0 < w_hi_last && p0 + kTile > w_lo_first;
+    const bool active = live && p0 < w_last.hi && p0 + kTile > w_first.lo;
     f32x16 S[2];
     if (active) {
 #pragma unroll
@@ -200,8 +142,8 @@ __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) 
         for (int s = 0; s < DH / 16; ++s)
           S[i] = mfma_32x32x16<E>(*reinterpret_cast<const uint4*>(&Kt[key_piece<DH>(i * 32 + col, 2 * s + half)]), qf[s], S[i]);
       }
-      const bool masked = p0 < w_lo_last || p0 + kTile > w_hi_first;
-      const uint32_t from = (uint32_t)(p0 + 4 * half - lo), len = hi > lo ? (uint32_t)(hi - lo) : 0u;
+      const bool masked = p0 < w_last.lo || p0 + kTile > w_first.hi;
+      const uint32_t from = (uint32_t)(p0 + 4 * half - lo);
       f32x16 inv[2];
       float mx = -INFINITY;
 #pragma unroll
@@ -242,13 +184,13 @@ __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) 
     // ---- infinities and NaN among the values of positions that some rows of the tile do not see: a weight of 0 would
     // still make NaN of them.  They are added to the rows that see them, and zeros take their places. ----
     if constexpr (PT == kPages16) {
-      if (p0 < wg_lo_last || p0 + kTile > wg_hi_first) {
+      if (p0 < wg_last.lo || p0 + kTile > wg_first.hi) {
         bool found = false;
         for (int e = tid; e < kTile * PIECES; e += NT) found = found || has_special<T>(*reinterpret_cast<const uint4*>(&Vt[e * 8]));
         if (__syncthreads_or(found)) {
           if (active)
             for (int j = 0; j < kTile; ++j) {
-              if ((uint32_t)(p0 + j - lo) >= (hi > lo ? (uint32_t)(hi - lo) : 0u)) continue;
+              if ((uint32_t)(p0 + j - lo) >= len) continue;
 #pragma unroll
               for (int jj = 0; jj < DH / 32; ++jj)
 #pragma unroll
@@ -301,8 +243,7 @@ __global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) 
       *reinterpret_cast<uint2*>(op + 32 * j + 8 * q + 4 * half) = none ? make_uint2(0u, 0u) : w;
     }
   if (a.lse && half == 0) {
-    const int64_t at = packed ? (int64_t)head * p.n_rows + r.row0 + t : ((int64_t)b * p.H + head) * p.n + t;
-    a.lse[at] = none ? -INFINITY : (m_ref + log2f(l)) * 0.6931471805599453f;
+    a.lse[lse_place(a, r, b, head, t)] = none ? -INFINITY : (m_ref + log2f(l)) * kLn2;
   }
 }
 
@@ -336,7 +277,7 @@ hipError_t launch_t(const PagedAttendArgs& a, int page_type, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_paged_attend(const PagedAttendArgs& a, int dtype, int page_type, hipStream_t s) {
+hipError_t launch_paged_chunk(const PagedAttendArgs& a, int dtype, int page_type, hipStream_t s) {
   return dtype == 1 ? launch_t<BF16>(a, page_type, s) : launch_t<F16>(a, page_type, s);
 }
 
