@@ -364,7 +364,8 @@ int sparq_paged_read(const sparq_paged_shape* shape, const sparq_paged_cache* ca
  * Positions that a row does not see have no part in its result, whatever they hold.  A row that sees nothing (a sequence of
  * length 0; one that starts before position 0), or only logits of -inf, is zeros with a logarithm of -inf; infinities and NaN among what it sees take their
  * course.  Sums and the softmax's state are fp32, weights are rounded to 16 bits before the product with the values (fp16 for 8-bit
- * pages), y is rounded to nearest-even.
+ * pages), y is rounded to nearest-even.  The same call gives the same bits every time; the order of a sequence's sums, and with it their
+ * last bits, goes by the lengths of the whole batch.
  *   q, out   device [.., H, .., d_h], dtype, 16-byte aligned; each with strides of its own; out must not overlap q
  *   lse_out  device fp32 or NULL: the natural logarithm of the softmax's denominator, [B, H, n], or with row_start [H, n_rows]
  * A length outside [0, S_bound] counts as 0 (SPARQ_ERR_BAD_SEQ_LEN); a page id outside the pool is taken as page 0

@@ -38,7 +38,6 @@ struct PagedAttendArgs {
   RowStrides qs, os;
   int32_t window, all;                                  // all: not causal
   int32_t group;                                        // query heads per KV head
-  int32_t n_tiles;                                      // row tiles per (sequence, KV head)
   int32_t skip_rows;                                    // sequences of up to this many rows (times group) are another launch's
   Divider by_group;
 };
@@ -92,9 +91,18 @@ constexpr int tokens_rows(int d_h) { return d_h == 64 ? 64 : (d_h == 128 ? 32 : 
 constexpr int tokens_per_cu(int d_h, int page_type) { return d_h == 256 && page_type == kPages16 ? 1 : 2; }
 constexpr int kTokensWorkgroups = 512;                  // at most
 
+// Many rows per (sequence, KV head): row tiles of chunk_rows rows.
+constexpr int chunk_rows = 128;
+constexpr int chunk_per_cu(int d_h) { return d_h == 256 ? 1 : 2; }
+struct ChunkPlan {
+  int workgroups;
+  float* partials;                                      // [workgroups][2][2 chunk_rows lanes][d_h / 2 + 4]
+  int32_t* tickets;                                     // [workgroups], 0 between launches
+};
+
 hipError_t launch_paged_append(const PagedRowsArgs& a, int dtype, int page_type, hipStream_t s);
 hipError_t launch_paged_read(const PagedRowsArgs& a, int dtype, int page_type, hipStream_t s);
-hipError_t launch_paged_chunk(const PagedAttendArgs& a, int dtype, int page_type, hipStream_t s);
+hipError_t launch_paged_chunk(const PagedAttendArgs& a, const ChunkPlan& c, int dtype, int page_type, hipStream_t s);
 hipError_t launch_paged_tokens(const PagedAttendArgs& a, const TokensPlan& t, int dtype, int page_type, hipStream_t s);
 
 }  // namespace sparq

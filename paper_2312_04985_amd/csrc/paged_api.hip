@@ -76,11 +76,23 @@ int tokens_workgroups(const sparq_paged_shape* s) {
   return (int)(units * 64 < most ? units * 64 : most);
 }
 
-// (calls of fewer rows than n need no more: they have at most as many rows per KV head as are counted here)
+// Workgroups of the second kernel: what runs at once, and no more than could have work (a row tile, and 4 tiles of positions of one).
+int chunk_workgroups(const sparq_paged_shape* s, int n) {
+  const int64_t rows = (int64_t)n * (s->H / s->H_kv), bound = s->S_bound > 0 ? s->S_bound : (int64_t)s->max_pages * s->page_size;
+  const int64_t tiles = (int64_t)s->B * s->H_kv * ((rows + chunk_rows - 1) / chunk_rows), most = 256 * chunk_per_cu(s->d_h);
+  const int64_t could = tiles * (bound / 256 + 1);
+  return (int)(could < most ? could : most);
+}
+
+// Scratch behind the control block; the two kernels of a call follow each other and share it.
+size_t tokens_scratch(const sparq_paged_shape* s, int rows) { return (size_t)tokens_workgroups(s) * 2 * tokens_tile(rows) * (s->d_h + 4) * sizeof(float); }
+size_t chunk_scratch(const sparq_paged_shape* s, int n) { return (size_t)chunk_workgroups(s, n) * 2 * (2 * chunk_rows) * (s->d_h / 2 + 4) * sizeof(float); }
+
+// (calls of fewer rows than n need no more: they have at most as many rows per KV head, and row tiles, as are counted here)
 size_t paged_workspace(const sparq_paged_shape* s, int n) {
   const int64_t rows = (int64_t)n * (s->H / s->H_kv), most = tokens_rows(s->d_h);
-  const int tile = tokens_tile((int)(rows < most ? rows : most));
-  return (size_t)kControlBytes + (size_t)tokens_workgroups(s) * 2 * tile * (s->d_h + 4) * sizeof(float);
+  const size_t first = tokens_scratch(s, (int)(rows < most ? rows : most)), second = rows > most ? chunk_scratch(s, n) : 0;
+  return (size_t)kControlBytes + (first > second ? first : second);
 }
 
 // everything that the calls have in common
@@ -165,7 +177,11 @@ int sparq_paged_attention(const sparq_paged_shape* shape, const sparq_paged_cach
     e = launch_paged_tokens(a, t, shape->dtype, shape->page_type, s);
   }
   a.skip_rows = plan.tokens_rows;
-  if (e == hipSuccess && plan.chunk) e = launch_paged_chunk(a, shape->dtype, shape->page_type, s);
+  if (e == hipSuccess && plan.chunk) {
+    const ChunkPlan c{chunk_workgroups(shape, rows->n), reinterpret_cast<float*>(static_cast<char*>(workspace) + kControlBytes),
+                      reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kTicketOffset)};
+    e = launch_paged_chunk(a, c, shape->dtype, shape->page_type, s);
+  }
   return e == hipSuccess ? SPARQ_OK : SPARQ_ELAUNCH;
 }
 

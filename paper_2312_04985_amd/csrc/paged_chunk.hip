@@ -1,6 +1,6 @@
 // Attention of many rows per (sequence, KV head) over a paged cache: chunks of new tokens, whole prompts.
 //
-// A workgroup serves 32 rows per wave of one (sequence, KV head): row m stands for token m / g and query head m % g of the
+// A workgroup's row tile is 32 rows per wave of one (sequence, KV head): row m stands for token m / g and query head m % g of the
 // group, so that the heads of a group share what is read of the cache.  It walks the positions that its rows see in tiles
 // of 64 through LDS, one pass, with the running maximum and sum of the softmax.
 //   scores   S^T[position][row] = K Q^T by 32x32x16 matrix instructions: a lane then holds 32 scores of ONE row, so that
@@ -9,14 +9,19 @@
 //            contraction runs over the positions in the order (8 a + 4 h + j), a = 0, 1, j = 0 .. 3 of lane half h
 //   output   O^T[channel][row] += V^T P^T; V^T comes out of LDS by the transposing load, in the same order of positions.
 // 8-bit pages: every code is a 16-bit float, so the products are those of 16-bit pages; a key's scale multiplies its scores.
-// A value's scale goes into the exponent: w_j = 2^(x_j + log2 s_j - m) <= 1 is what multiplies the codes, and w_j / s_j what
+// A value's scale goes into the exponent: w_j = 2^(x_j + log2 s_j - m) is what multiplies the codes, and w_j / s_j what
 // is summed.  Neither needs a rounding that 16-bit pages do not have.
+//
+// The work of the whole batch is one line of (sequence, KV head, row tile, tile of 64 positions) in order, cut into equal parts,
+// one per workgroup: chunks of different lengths, a causal mask's unequal row tiles and few rows over a long cache all load the
+// chip evenly.  A row tile that several workgroups share is put together by the last of them to finish.
 #include "paged_core.h"
 
 namespace sparq {
 namespace {
 
 constexpr int kTile = 64;               // positions per tile
+constexpr int kWaves = chunk_rows / 32; // waves of a workgroup
 
 // c[m][n] += sum_k a[m][k] b[n][k] over 16 k: lane l holds a[l % 32], b[l % 32] at k = 8 (l / 32) .. + 7 and
 // c[8 (i / 4) + 4 (l / 32) + i % 4][l % 32]
@@ -30,255 +35,433 @@ template <> __device__ __forceinline__ f32x16 mfma_32x32x16<BF16>(const uint4& a
 
 // Rows of DH elements in LDS in pieces of 8 (16 bytes).  Keys are read by 32 rows at one piece, values by 8 rows at 4
 // neighbouring pieces: both are spread over the banks by changing the pieces' places with the row.
-template <int DH> __device__ __forceinline__ int key_piece(int row, int piece) { return row * DH + ((piece ^ (row & (DH / 8 - 1) & 15)) << 3); }
-template <int DH> __device__ __forceinline__ int value_piece(int row, int piece) {
-  const int turn = DH == 64 ? ((row & 1) << 2) | ((row >> 1) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
-  return row * DH + ((piece ^ turn) << 3);
+template <int DH> __device__ __forceinline__ int key_turn(int row) { return row & (DH / 8 - 1) & 15; }
+template <int DH> __device__ __forceinline__ int value_turn(int row) { return DH == 64 ? ((row & 1) << 2) | ((row >> 1) & 3) : ((row & 3) << 2) | ((row >> 2) & 3); }
+template <int DH> __device__ __forceinline__ int key_piece(int row, int piece) { return row * DH + ((piece ^ key_turn<DH>(row)) << 3); }
+template <int DH> __device__ __forceinline__ int value_piece(int row, int piece) { return row * DH + ((piece ^ value_turn<DH>(row)) << 3); }
+
+// 16 bytes per lane from memory into LDS at `to` + 16 lane, without a way through registers
+__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
+  typedef __attribute__((address_space(1))) const void gvoid;
+  typedef __attribute__((address_space(3))) void lvoid;
+  __builtin_amdgcn_global_load_lds((gvoid*)from, (lvoid*)to, 16, 0, 0);
 }
 
-template <class T, int PT, int DH, int NW>
-__global__ __launch_bounds__(NW * 64) void paged_chunk(const PagedAttendArgs a) {
-  using E = Product<T, PT>;
-  constexpr int NT = NW * 64, ROWS = NW * 32, PIECES = DH / 8;
-  __shared__ __align__(16) uint16_t Kt[kTile * DH], Vt[kTile * DH];
-  __shared__ __align__(16) float s_k[kTile], s_log[kTile], s_inv[kTile];   // 8-bit pages: scale of the key, log2 and inverse of the value's
-  const PagedArgs& p = a.p;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+// All of this wave's loads have arrived and its LDS accesses are done; then all waves' have.
+__device__ __forceinline__ void tile_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
-  // Workgroups are dealt round-robin to the 8 XCDs: eight (sequence, KV head) units at a time, so that the workgroups that
-  // share rows of the cache share an XCD's L2; a unit's last row tiles, which see most, first.
-  const int units = p.B * p.H_kv, chunk = blockIdx.x / (8 * a.n_tiles), in_chunk = blockIdx.x - chunk * 8 * a.n_tiles;
-  const int width = units - chunk * 8 < 8 ? units - chunk * 8 : 8;
-  const int tile_up = in_chunk / width, unit = chunk * 8 + in_chunk - tile_up * width, tile = a.n_tiles - 1 - tile_up;
-  const int b = divided(unit, p.by_H_kv), hk = unit - b * p.H_kv;
-  const SeqRows r = seq_rows(p.seq_lens[b], p.bound, p.n, p.n_per_seq, p.row_start, p.n_rows, b);
-  if (r.err && tid == 0 && hk == 0 && tile == 0) atomicOr(p.err, r.err);
-  const int M = r.n * a.group, m0 = tile * ROWS;
-  if (m0 >= M || M <= a.skip_rows) return;
+template <class T, int PT, int DH>
+__global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(const PagedAttendArgs a, const int G, const Divider by_G, float* partials, int32_t* tickets) {
+  using E = Product<T, PT>;
+  constexpr int NW = kWaves, NTH = NW * 64, ROWS = NW * 32, PIECES = DH / 8, ND = DH / 32;
+  constexpr int GW = NW / 4;                                   // waves that load one group of 16 positions
+  constexpr int LOADS = 16 * PIECES / 64 / GW;                 // 16-bit pages: loads of 1 KB per wave, keys and values each
+  constexpr int CL = PT == kPages16 ? 1 : (DH / 64 / GW > 0 ? DH / 64 / GW : 1);   // 8-bit pages: loads of 16 codes per lane
+  static_assert(NW == 4 || (NW == 8 && DH >= 128), "whole loads");
+  __shared__ __align__(16) uint16_t Kt[2][kTile * DH], Vt[2][kTile * DH];
+  __shared__ __align__(16) float s_k[2][kTile], s_log[2][kTile], s_inv[2][kTile];   // 8-bit pages: scale of the key, log2 and inverse of the value's
+  __shared__ int64_t sum_w[NW];
+  __shared__ int s_begin[4];
+  __shared__ int flag;
+  const PagedArgs& p = a.p;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const bool packed = p.row_start != nullptr;
 
-  const int m_w = m0 + wave * 32, m_last = M - 1;
-  const bool live = m_w < M;                                   // a wave without rows only helps to load
-  const int m = m_w + col < M ? m_w + col : m_last;
-  const int t = divided(m, a.by_group), head = hk * a.group + m - t * a.group;
-  const auto row_sees = [&](int m) { return seen_by(a, r, divided(m < M ? m : m_last, a.by_group)); };
-  const Seen mine = seen_by(a, r, t), wg_first = row_sees(m0), wg_last = row_sees(m0 + ROWS - 1), w_first = row_sees(m_w), w_last = row_sees(m_w + 31);
-  const int lo = mine.lo;
-  const uint32_t len = mine.hi > lo ? (uint32_t)(mine.hi - lo) : 0u;
-
-  // the lane's part of its row of Q: channels 16 s + 8 half .. + 7
-  uint4 qf[DH / 16];
-  const uint16_t* qp = reinterpret_cast<const uint16_t*>(a.q) + row_offset(a.qs, packed, b, r.row0, head, t) + half * 8;
+  // ---- this workgroup's part of the line ----
+  auto rows_of = [&](int b) { return seq_rows(p.seq_lens[b], p.bound, p.n, p.n_per_seq, p.row_start, p.n_rows, b); };
+  auto tiles_of = [&](const SeqRows& r) { const int M = r.n * a.group; return M <= a.skip_rows ? 0 : (M + ROWS - 1) / ROWS; };
+  // tiles of 64 positions that row tile k sees, from position `from` on (one at least: rows that see nothing are written too)
+  auto steps_of = [&](const SeqRows& r, int k, int& from, int& to) {
+    const int M = r.n * a.group, m0 = k * ROWS, m1 = m0 + ROWS < M ? m0 + ROWS : M;
+    from = seen_by(a, r, divided(m0, a.by_group)).lo & ~(kTile - 1);
+    to = seen_by(a, r, divided(m1 - 1, a.by_group)).hi;
+    return to - from <= kTile ? 1 : (to - from + kTile - 1) / kTile;
+  };
+  auto steps_of_unit = [&](const SeqRows& r) -> int64_t {      // by all lanes of a wave together
+    const int n_tiles = tiles_of(r);
+    int64_t sum = 0;
+    int from, to;
+    for (int k = lane; k < n_tiles; k += kWave) sum += steps_of(r, k, from, to);
 #pragma unroll
-  for (int s = 0; s < DH / 16; ++s) qf[s] = *reinterpret_cast<const uint4*>(qp + s * 16);
-  float c_row = kLog2e / sqrtf((float)DH);                     // scores to exponents of 2
-  if constexpr (PT != kPages16 && std::is_same_v<T, BF16>) query_to_half<32>(qf, c_row);
-
-  f32x16 O[DH / 32];
+    for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o);
+    return sum;
+  };
+  // Consecutive parts of the line share rows of the cache; so that they share an L2 too, each of the 8 XCDs, which workgroups are dealt
+  // to round-robin, takes an eighth of the line.
+  const int me = G % 8 == 0 ? (int)(blockIdx.x % 8) * (G / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
+  const int per = (p.B + NW - 1) / NW, b_first = wave * per, b_last = b_first + per < p.B ? b_first + per : p.B;
+  int64_t mine = 0;
+  for (int b = b_first; b < b_last; ++b) {
+    const SeqRows r = rows_of(b);
+    if (r.err && me == 0 && lane == 0) atomicOr(p.err, r.err);
+    mine += steps_of_unit(r);
+  }
+  if (lane == 0) sum_w[wave] = mine;
+  __syncthreads();
+  int64_t before = 0, total = 0;
 #pragma unroll
-  for (int j = 0; j < DH / 32; ++j)
+  for (int w = 0; w < NW; ++w) { before += w < wave ? sum_w[w] : 0; total += sum_w[w]; }
+  before *= p.H_kv; total *= p.H_kv;
+  const int64_t share = total < INT32_MAX - G ? (int64_t)divided((int)total + G - 1, by_G) : (total + G - 1) / G;
+  const int64_t begin = (int64_t)me * share, end = begin + share < total ? begin + share : total;
+  if (begin >= end) return;
+  if (before <= begin && begin < before + mine * p.H_kv) {     // one wave
+    int64_t at = before, c = 1;
+    int b = b_first;
+    for (; b < b_last; ++b) {
+      c = steps_of_unit(rows_of(b));
+      if (begin < at + c * p.H_kv || b == b_last - 1) break;
+      at += c * p.H_kv;
+    }
+    const int64_t off = begin - at;
+    const int hk = (int)(off / (c > 0 ? c : 1));
+    int64_t rest = off - hk * c;
+    const SeqRows r = rows_of(b);
+    const int n_tiles = tiles_of(r);
+    for (int k0 = 0; k0 < n_tiles; k0 += kWave) {
+      int from, to;
+      const uint32_t cnt = k0 + lane < n_tiles ? (uint32_t)steps_of(r, k0 + lane, from, to) : 0u;
+      uint32_t upto = cnt;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) O[j][i] = 0.0f;
-  float m_ref = -INFINITY, l = 0.0f;
+      for (int o = 1; o < kWave; o <<= 1) { const uint32_t x = __shfl_up(upto, o); if (lane >= o) upto += x; }
+      const uint64_t past = __ballot((int64_t)upto > rest);
+      if (past) {
+        if (lane == __builtin_ctzll(past)) { s_begin[0] = b; s_begin[1] = hk; s_begin[2] = k0 + lane; s_begin[3] = (int)(rest - (upto - cnt)); }
+        break;
+      }
+      rest -= __shfl(upto, 63);
+    }
+  }
+  __syncthreads();
+  int b = __builtin_amdgcn_readfirstlane(s_begin[0]), hk = __builtin_amdgcn_readfirstlane(s_begin[1]), tile = __builtin_amdgcn_readfirstlane(s_begin[2]),
+      skip = __builtin_amdgcn_readfirstlane(s_begin[3]);        // steps of the first row tile that are others'
 
-  const int begin = wg_first.lo / kTile * kTile;
-  for (int p0 = begin; p0 < wg_last.hi; p0 += kTile) {
-    // ---- the tile into LDS: 16 rows of a page per turn of a wave ----
-    for (int g = wave; g < kTile / 16; g += NW) {
-      const int pos0 = p0 + g * 16;
-      const int at = pos0 < r.S ? pos0 : 0;                    // (behind the last position: any row, its values are not used)
-      const int index = divided(at, p.by_page);
+  for (int64_t at = begin; at < end;) {
+    const SeqRows r = rows_of(b);
+    const int n_tiles = tiles_of(r);
+    if (tile >= n_tiles) {                                     // the next KV head or sequence (one with rows follows: at < end <= total)
+      tile = 0;
+      if (n_tiles == 0 || ++hk == p.H_kv) { hk = 0; if (++b >= p.B) return; }
+      continue;
+    }
+    int from, to;
+    const int steps = steps_of(r, tile, from, to);
+    const int todo = (int)(end - at < steps - skip ? end - at : steps - skip);
+    const int64_t tile_at = at - skip;
+
+    // ---- the lane's row ----
+    const int M = r.n * a.group, m0 = tile * ROWS, m_w = m0 + wave * 32, m_last = M - 1;
+    const bool live = m_w < M;                                 // a wave without rows only helps to load
+    const int m = m_w + col < M ? m_w + col : m_last;
+    const int t = divided(m, a.by_group), head = hk * a.group + m - t * a.group;
+    const auto row_sees = [&](int x) { return seen_by(a, r, divided(x < M ? x : m_last, a.by_group)); };
+    const Seen mine_sees = seen_by(a, r, t), wg_first = row_sees(m0), wg_last = row_sees(m0 + ROWS - 1), w_first = row_sees(m_w), w_last = row_sees(m_w + 31);
+    const int lo = mine_sees.lo;
+    const uint32_t len = mine_sees.hi > lo ? (uint32_t)(mine_sees.hi - lo) : 0u;
+
+    // its part of the row of Q: channels 16 s + 8 half .. + 7
+    uint4 qf[DH / 16];
+    const uint16_t* qp = reinterpret_cast<const uint16_t*>(a.q) + row_offset(a.qs, packed, b, r.row0, head, t) + half * 8;
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s) qf[s] = *reinterpret_cast<const uint4*>(qp + s * 16);
+    float c_row = kLog2e / sqrtf((float)DH);                   // scores to exponents of 2
+    if constexpr (PT != kPages16 && std::is_same_v<T, BF16>) query_to_half<32>(qf, c_row);
+
+    f32x16 O[ND];
+#pragma unroll
+    for (int j = 0; j < ND; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) O[j][i] = 0.0f;
+    float m_ref = -INFINITY, l = 0.0f;
+
+    // ---- loads: a wave's part of a tile is 16 positions, which share a page ----
+    const int p_begin = from + skip * kTile, p_end = from + (skip + todo) * kTile < to ? from + (skip + todo) * kTile : to;
+    const int group = wave / GW, part = wave % GW;
+    auto place = [&](int p0) -> int64_t {
+      const int pos0 = p0 + group * 16, x = pos0 < to ? pos0 : from;   // (behind the last position: any row, its values are not used)
+      const int index = divided(x, p.by_page);
       int page = page_at(p, b, index);
       if (page < 0) { if (lane == 0) atomicOr(p.err, kErrBadPage); page = 0; }
-      const int64_t row = pool_row(p, page, hk, at - index * p.page_size);
+      return pool_row(p, page, hk, x - index * p.page_size);
+    };
+    uint4 ck[CL], cv[CL];                                      // 8-bit pages: the next tile's codes and scales
+    float csk = 0.0f, csv = 0.0f;
+    auto issue = [&](int64_t row, int buf) {
       if constexpr (PT == kPages16) {
         const uint16_t* kp = reinterpret_cast<const uint16_t*>(p.K) + row * DH;
         const uint16_t* vp = reinterpret_cast<const uint16_t*>(p.V) + row * DH;
 #pragma unroll
-        for (int i = 0; i < 16 * PIECES / 64; ++i) {
-          const int e = i * 64 + lane, rr = e / PIECES, piece = e % PIECES;
-          const uint4 k = *reinterpret_cast<const uint4*>(kp + e * 8);
-          uint4 v = *reinterpret_cast<const uint4*>(vp + e * 8);
-          if (pos0 + rr >= r.S) v = make_uint4(0, 0, 0, 0);
-          *reinterpret_cast<uint4*>(&Kt[key_piece<DH>(g * 16 + rr, piece)]) = k;
-          *reinterpret_cast<uint4*>(&Vt[value_piece<DH>(g * 16 + rr, piece)]) = v;
+        for (int i = 0; i < LOADS; ++i) {
+          const int e = (part * LOADS + i) * 64 + lane, rr = group * 16 + e / PIECES, slot = e % PIECES, at8 = (group * 16 * PIECES + (part * LOADS + i) * 64) * 8;
+          load_to_lds(kp + (e / PIECES) * DH + (slot ^ key_turn<DH>(rr)) * 8, &Kt[buf][at8]);
+          load_to_lds(vp + (e / PIECES) * DH + (slot ^ value_turn<DH>(rr)) * 8, &Vt[buf][at8]);
         }
       } else {
         const uint8_t* kp = reinterpret_cast<const uint8_t*>(p.K) + row * DH;
         const uint8_t* vp = reinterpret_cast<const uint8_t*>(p.V) + row * DH;
 #pragma unroll
-        for (int i = 0; i < 16 * PIECES / 64; ++i) {
-          const int e = i * 64 + lane, rr = e / PIECES, piece = e % PIECES;
-          const uint2 k = *reinterpret_cast<const uint2*>(kp + e * 8);
-          uint2 v = *reinterpret_cast<const uint2*>(vp + e * 8);
-          uint2 x = codes_to_half<PT>(k.x), y = codes_to_half<PT>(k.y);
-          *reinterpret_cast<uint4*>(&Kt[key_piece<DH>(g * 16 + rr, piece)]) = make_uint4(x.x, x.y, y.x, y.y);
-          x = codes_to_half<PT>(v.x); y = codes_to_half<PT>(v.y);
-          uint4 w = make_uint4(x.x, x.y, y.x, y.y);
-          if (pos0 + rr >= r.S) w = make_uint4(0, 0, 0, 0);
-          *reinterpret_cast<uint4*>(&Vt[value_piece<DH>(g * 16 + rr, piece)]) = w;
+        for (int i = 0; i < CL; ++i) {
+          const int e = (part * CL + i) * 64 + lane;           // 16 codes each
+          ck[i] = *reinterpret_cast<const uint4*>(kp + e * 16);
+          cv[i] = *reinterpret_cast<const uint4*>(vp + e * 16);
         }
-        if (lane < 16) {
-          const float sk = p.K_scale[row + lane], sv = p.V_scale[row + lane];
-          const float v = value_scale(sv);
-          s_k[g * 16 + lane] = sk;
-          s_log[g * 16 + lane] = log2_normal(v);
-          s_inv[g * 16 + lane] = 1.0f / v;
+        if (part == 0) { csk = p.K_scale[row + (lane & 15)]; csv = p.V_scale[row + (lane & 15)]; }
+      }
+    };
+    auto settle = [&](int p0, int buf) {                       // 8-bit pages: codes that have arrived go to LDS as fp16
+      if constexpr (PT != kPages16) {
+        auto put = [&](uint16_t* dst0, uint16_t* dst1, const uint4& w, bool on) {
+          const uint2 x0 = codes_to_half<PT>(on ? w.x : 0u), x1 = codes_to_half<PT>(on ? w.y : 0u), x2 = codes_to_half<PT>(on ? w.z : 0u), x3 = codes_to_half<PT>(on ? w.w : 0u);
+          *reinterpret_cast<uint4*>(dst0) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+          *reinterpret_cast<uint4*>(dst1) = make_uint4(x2.x, x2.y, x3.x, x3.y);
+        };
+#pragma unroll
+        for (int i = 0; i < CL; ++i) {
+          const int e = (part * CL + i) * 64 + lane, rr = group * 16 + e / (DH / 16), piece = e % (DH / 16) * 2;
+          put(&Kt[buf][key_piece<DH>(rr, piece)], &Kt[buf][key_piece<DH>(rr, piece + 1)], ck[i], true);
+          put(&Vt[buf][value_piece<DH>(rr, piece)], &Vt[buf][value_piece<DH>(rr, piece + 1)], cv[i], p0 + rr < to);
+        }
+        if (part == 0 && lane < 16) {
+          const float v = value_scale(csv);
+          s_k[buf][group * 16 + lane] = csk;
+          s_log[buf][group * 16 + lane] = log2_normal(v);
+          s_inv[buf][group * 16 + lane] = 1.0f / v;
         }
       }
-    }
-    __syncthreads();
+    };
 
-    // ---- scores, exponents, weights ----
-    // (a row's exponent of 2 at position j is x_j = c q . K_j, with 8-bit pages plus log2 s_j)
-    const bool active = live && p0 < w_last.hi && p0 + kTile > w_first.lo;
-    f32x16 S[2];
-    if (active) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) S[i][e] = 0.0f;
-#pragma unroll
-        for (int s = 0; s < DH / 16; ++s)
-          S[i] = mfma_32x32x16<E>(*reinterpret_cast<const uint4*>(&Kt[key_piece<DH>(i * 32 + col, 2 * s + half)]), qf[s], S[i]);
-      }
-      const bool masked = p0 < w_last.lo || p0 + kTile > w_first.hi;
-      const uint32_t from = (uint32_t)(p0 + 4 * half - lo);
-      f32x16 inv[2];
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = 32 * i + 8 * (e / 4) + e % 4, at = j + 4 * half;
-          float x;
-          if constexpr (PT == kPages16) x = S[i][e] * c_row;
-          else { x = fmaf(S[i][e], s_k[at] * c_row, s_log[at]); inv[i][e] = s_inv[at]; }
-          if (masked && from + j >= len) { x = -INFINITY; if constexpr (PT != kPages16) inv[i][e] = 0.0f; }
-          S[i][e] = x;
-          mx = fmaxf(mx, x);
-        }
-      float m_a, m_b;
-      lane_pair<32>(mx, m_a, m_b);
-      const float m_new = fmaxf(fmaxf(m_a, m_b), m_ref);
-      if (__ballot(m_new > m_ref)) {
-        const float w = weight_exp2(m_ref, m_new);
-        m_ref = m_new;
-        l *= w;
-#pragma unroll
-        for (int j = 0; j < DH / 32; ++j)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) O[j][e] *= w;
-      }
-      const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;     // (nothing seen yet: every weight is 2^-inf)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          S[i][e] = exp2_weight(S[i][e] - m_use);
-          if constexpr (PT == kPages16) l += S[i][e];
-          else l = fmaf(S[i][e], inv[i][e], l);
-        }
+    int64_t row_next = 0;
+    if (p_begin < p_end) {
+      issue(place(p_begin), 0);
+      settle(p_begin, 0);
+      row_next = place(p_begin + kTile);
     }
+    for (int p0 = p_begin, buf = 0; p0 < p_end; p0 += kTile, buf ^= 1) {
+      tile_barrier();                                          // this tile is there; nobody reads the other buffer
+      const bool more = p0 + kTile < p_end;
+      if (more) issue(row_next, buf ^ 1);
+      row_next = place(p0 + 2 * kTile);
+      uint16_t* const kt = Kt[buf];
+      uint16_t* const vt = Vt[buf];
+      if constexpr (PT == kPages16) {
+        if (p0 + kTile > to) {                                 // values behind the last position: zeros
+          for (int e = tid; e < (p0 + kTile - to) * PIECES; e += NTH) *reinterpret_cast<uint4*>(&vt[(to - p0) * DH + e * 8]) = make_uint4(0, 0, 0, 0);
+          __syncthreads();
+        }
+      }
 
-    // ---- infinities and NaN among the values of positions that some rows of the tile do not see: a weight of 0 would
-    // still make NaN of them.  They are added to the rows that see them, and zeros take their places. ----
-    if constexpr (PT == kPages16) {
-      if (p0 < wg_last.lo || p0 + kTile > wg_first.hi) {
-        bool found = false;
-        for (int e = tid; e < kTile * PIECES; e += NT) found = found || has_special<T>(*reinterpret_cast<const uint4*>(&Vt[e * 8]));
-        if (__syncthreads_or(found)) {
-          if (active)
-            for (int j = 0; j < kTile; ++j) {
-              if ((uint32_t)(p0 + j - lo) >= len) continue;
+      // ---- scores, exponents, weights ----
+      // (a row's exponent of 2 at position j is x_j = c q . K_j, with 8-bit pages plus log2 s_j)
+      const bool active = live && p0 < w_last.hi && p0 + kTile > w_first.lo;
+      f32x16 S[2];
+      if (active) {
 #pragma unroll
-              for (int jj = 0; jj < DH / 32; ++jj)
+        for (int i = 0; i < 2; ++i) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const int d = 32 * jj + 8 * (e / 4) + 4 * half + e % 4;
-                  const float v = T::widen(Vt[value_piece<DH>(j, d / 8) + d % 8]);
-                  if (!(fabsf(v) < INFINITY)) O[jj][e] += v;
-                }
+          for (int e = 0; e < 16; ++e) S[i][e] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < DH / 16; ++s)
+            S[i] = mfma_32x32x16<E>(*reinterpret_cast<const uint4*>(&kt[key_piece<DH>(i * 32 + col, 2 * s + half)]), qf[s], S[i]);
+        }
+        if constexpr (PT != kPages16) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int j = 32 * i + 8 * (e / 4) + e % 4 + 4 * half;
+              S[i][e] = fmaf(S[i][e], s_k[buf][j] * c_row, s_log[buf][j]);
             }
-          __syncthreads();
-          for (int e = tid; e < kTile * DH; e += NT)
-            if (!(fabsf(T::widen(Vt[e])) < INFINITY)) Vt[e] = 0;
-          __syncthreads();
+        }
+        const bool masked = p0 < w_last.lo || p0 + kTile > w_first.hi;
+        const uint32_t at0 = (uint32_t)(p0 + 4 * half - lo);
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (at0 + (32 * i + 8 * (e / 4) + e % 4) >= len) S[i][e] = -INFINITY;
+        }
+        const float c = PT == kPages16 ? c_row : 1.0f;         // (8-bit pages: in the exponents already)
+        float mx = fmaxf(S[0][0], S[1][0]);
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(fmaxf(mx, S[0][e]), S[1][e]);
+        float m_a, m_b;
+        lane_pair<32>(mx, m_a, m_b);
+        const float m_new = fmaxf(m_a, m_b) * c;
+        // the maximum is followed only when it rises by more than 8: weights are at most 2^8 then, and most tiles rescale nothing
+        if (__ballot(m_new > m_ref + 8.0f)) {
+          const float m_to = fmaxf(m_new, m_ref);
+          const float w = weight_exp2(m_ref, m_to);
+          m_ref = m_to;
+          l *= w;
+#pragma unroll
+          for (int j = 0; j < ND; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) O[j][e] *= w;
+        }
+        const float m_use = m_ref == -INFINITY ? 0.0f : m_ref; // (nothing seen yet: every weight is 2^-inf)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) S[i][e] = exp2_weight(PT == kPages16 ? fmaf(S[i][e], c, -m_use) : S[i][e] - m_use);
+        if constexpr (PT == kPages16) {
+          float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) { l0 += S[0][e]; l1 += S[1][e]; }
+          l += l0 + l1;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int j = 32 * i + 8 * (e / 4) + e % 4;
+              float inv = s_inv[buf][j + 4 * half];
+              if (masked && at0 + j >= len) inv = 0.0f;        // (whatever the scale of a position that is not seen: 0 times it)
+              l = fmaf(S[i][e], inv, l);
+            }
+        }
+      }
+
+      // ---- infinities and NaN among the values of positions that some rows of the tile do not see: a weight of 0 would
+      // still make NaN of them.  They are added to the rows that see them, and zeros take their places. ----
+      if constexpr (PT == kPages16) {
+        if (p0 < wg_last.lo || p0 + kTile > wg_first.hi) {
+          bool found = false;
+          for (int e = tid; e < kTile * PIECES; e += NTH) found = found || has_special<T>(*reinterpret_cast<const uint4*>(&vt[e * 8]));
+          if (__syncthreads_or(found)) {
+            if (active)
+              for (int j = 0; j < kTile; ++j) {
+                if ((uint32_t)(p0 + j - lo) >= len) continue;
+#pragma unroll
+                for (int jj = 0; jj < ND; ++jj)
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) {
+                    const int d = 32 * jj + 8 * (e / 4) + 4 * half + e % 4;
+                    const float v = T::widen(vt[value_piece<DH>(j, d / 8) + d % 8]);
+                    if (!(fabsf(v) < INFINITY)) O[jj][e] += v;
+                  }
+              }
+            __syncthreads();
+            for (int e = tid; e < kTile * DH; e += NTH)
+              if (!(fabsf(T::widen(vt[e])) < INFINITY)) vt[e] = 0;
+            __syncthreads();
+          }
+        }
+      }
+
+      // ---- output ----
+      if (active) {
+#pragma unroll
+        for (int sl = 0; sl < 4; ++sl) {
+          const int e0 = sl % 2 * 8;
+          const f32x16& w = S[sl / 2];
+          const uint4 pw = make_uint4(narrow2<E>(w[e0], w[e0 + 1]), narrow2<E>(w[e0 + 2], w[e0 + 3]), narrow2<E>(w[e0 + 4], w[e0 + 5]), narrow2<E>(w[e0 + 6], w[e0 + 7]));
+          const int row = sl * 16 + 4 * half + (lane & 15) / 4;
+#pragma unroll
+          for (int j = 0; j < ND; ++j) {
+            const int piece = 4 * j + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), sub = (lane & 1) * 4;
+            const uint2 v0 = lds_read_transposed(&vt[value_piece<DH>(row, piece) + sub]), v1 = lds_read_transposed(&vt[value_piece<DH>(row + 8, piece) + sub]);
+            O[j] = mfma_32x32x16<E>(make_uint4(v0.x, v0.y, v1.x, v1.y), pw, O[j]);
+          }
+        }
+      }
+      if (more) settle(p0 + kTile, buf ^ 1);
+    }
+
+    // ---- a row tile that several workgroups share: partial results in the order of registers ----
+    const int64_t tile_end = tile_at + steps;
+    bool write = true;
+    if (skip != 0 || todo != steps) {
+      const int first_wg = skip == 0 ? me : (int)(tile_at / share), last_wg = tile_end <= end ? me : (int)((tile_end - 1) / share);
+      constexpr int SLOT = NTH * (DH / 2 + 4);                 // floats: a lane's DH / 2 numerators, its maximum and its part of the denominator
+      auto slot_of = [&](int wg) { return partials + ((size_t)wg * 2 + (wg == first_wg ? 1 : 0)) * SLOT; };
+      float* dst = slot_of(me);
+#pragma unroll
+      for (int j = 0; j < ND; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) store_agent4(dst, (uint32_t)((j * 4 + q) * NTH + tid) * 16, make_float4(O[j][4 * q], O[j][4 * q + 1], O[j][4 * q + 2], O[j][4 * q + 3]));
+      store_agent4(dst, (uint32_t)(ND * 4 * NTH + tid) * 16, make_float4(m_ref, l, 0.0f, 0.0f));
+      write = last_to_arrive(tickets + first_wg, last_wg - first_wg + 1, &flag);
+      if (write) {                                             // in the order of the line, whoever is last
+        m_ref = -INFINITY; l = 0.0f;
+#pragma unroll
+        for (int j = 0; j < ND; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[j][i] = 0.0f;
+        for (int wg = first_wg; wg <= last_wg; ++wg) {
+          const float* src = slot_of(wg);
+          const float4 st = load_agent4(src, (uint32_t)(ND * 4 * NTH + tid) * 16);
+          float4 o[ND * 4];
+#pragma unroll
+          for (int i = 0; i < ND * 4; ++i) o[i] = load_agent4(src, (uint32_t)(i * NTH + tid) * 16);
+          const float m_to = fmaxf(m_ref, st.x), f = weight_exp2(m_ref, m_to), g = weight_exp2(st.x, m_to);
+          m_ref = m_to;
+          l = l * f + st.y * g;
+#pragma unroll
+          for (int i = 0; i < ND * 4; ++i) {
+            O[i / 4][i % 4 * 4] = O[i / 4][i % 4 * 4] * f + o[i].x * g; O[i / 4][i % 4 * 4 + 1] = O[i / 4][i % 4 * 4 + 1] * f + o[i].y * g;
+            O[i / 4][i % 4 * 4 + 2] = O[i / 4][i % 4 * 4 + 2] * f + o[i].z * g; O[i / 4][i % 4 * 4 + 3] = O[i / 4][i % 4 * 4 + 3] * f + o[i].w * g;
+          }
         }
       }
     }
 
-    // ---- output ----
-    if (active) {
+    // ---- a row's two halves have summed half of its weights each ----
+    float l_a, l_b;
+    lane_pair<32>(l, l_a, l_b);
+    l = l_a + l_b;
+    if (write && live && m_w + col < M) {
+      const bool none = l == 0.0f;                             // nothing seen: zeros (a sum that is NaN stays NaN)
+      const float inv_l = none ? 0.0f : 1.0f / l;
+      uint16_t* op = reinterpret_cast<uint16_t*>(a.out) + row_offset(a.os, packed, b, r.row0, head, t);
 #pragma unroll
-      for (int sl = 0; sl < 4; ++sl) {
-        const int e0 = sl % 2 * 8;
-        const f32x16& w = S[sl / 2];
-        const uint4 pw = make_uint4(narrow2<E>(w[e0], w[e0 + 1]), narrow2<E>(w[e0 + 2], w[e0 + 3]), narrow2<E>(w[e0 + 4], w[e0 + 5]), narrow2<E>(w[e0 + 6], w[e0 + 7]));
-        const int row = sl * 16 + 4 * half + (lane & 15) / 4;
+      for (int j = 0; j < ND; ++j)
 #pragma unroll
-        for (int j = 0; j < DH / 32; ++j) {
-          const int piece = 4 * j + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), sub = (lane & 1) * 4;
-          const uint2 v0 = lds_read_transposed(&Vt[value_piece<DH>(row, piece) + sub]), v1 = lds_read_transposed(&Vt[value_piece<DH>(row + 8, piece) + sub]);
-          O[j] = mfma_32x32x16<E>(make_uint4(v0.x, v0.y, v1.x, v1.y), pw, O[j]);
+        for (int q = 0; q < 4; ++q) {
+          const uint2 w = make_uint2(narrow2<T>(O[j][4 * q] * inv_l, O[j][4 * q + 1] * inv_l), narrow2<T>(O[j][4 * q + 2] * inv_l, O[j][4 * q + 3] * inv_l));
+          *reinterpret_cast<uint2*>(op + 32 * j + 8 * q + 4 * half) = none ? make_uint2(0u, 0u) : w;
         }
-      }
+      if (a.lse && half == 0) a.lse[lse_place(a, r, b, head, t)] = none ? -INFINITY : (m_ref + log2f(l)) * kLn2;
     }
-    __syncthreads();                                             // the next tile overwrites this one
-  }
-
-  // ---- a row's two halves have summed half of its weights each ----
-  float l_a, l_b;
-  lane_pair<32>(l, l_a, l_b);
-  l = l_a + l_b;
-  if (!live || m_w + col >= M) return;
-  const bool none = l == 0.0f;                                   // nothing seen: zeros (a sum that is NaN stays NaN)
-  const float inv_l = none ? 0.0f : 1.0f / l;
-  uint16_t* op = reinterpret_cast<uint16_t*>(a.out) + row_offset(a.os, packed, b, r.row0, head, t);
-#pragma unroll
-  for (int j = 0; j < DH / 32; ++j)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint2 w = make_uint2(narrow2<T>(O[j][4 * q] * inv_l, O[j][4 * q + 1] * inv_l), narrow2<T>(O[j][4 * q + 2] * inv_l, O[j][4 * q + 3] * inv_l));
-      *reinterpret_cast<uint2*>(op + 32 * j + 8 * q + 4 * half) = none ? make_uint2(0u, 0u) : w;
-    }
-  if (a.lse && half == 0) {
-    a.lse[lse_place(a, r, b, head, t)] = none ? -INFINITY : (m_ref + log2f(l)) * kLn2;
+    at += todo;
+    skip = 0;
+    ++tile;
+    __syncthreads();                                           // (LDS is used anew)
   }
 }
 
 template <class T, int PT, int DH>
-hipError_t launch_one(const PagedAttendArgs& args, hipStream_t s) {
-  constexpr int NW = 4;
-  PagedAttendArgs a = args;
-  a.n_tiles = (int)(((int64_t)a.p.n * a.group + NW * 32 - 1) / (NW * 32));
-  const int64_t blocks = (int64_t)a.p.B * a.p.H_kv * a.n_tiles;
-  hipLaunchKernelGGL((paged_chunk<T, PT, DH, NW>), dim3((uint32_t)blocks), dim3(NW * 64), 0, s, a);
+hipError_t launch_one(const PagedAttendArgs& a, const ChunkPlan& c, hipStream_t s) {
+  hipLaunchKernelGGL((paged_chunk<T, PT, DH>), dim3(c.workgroups), dim3(kWaves * 64), 0, s, a, c.workgroups, make_divider(c.workgroups), c.partials, c.tickets);
   return hipGetLastError();
 }
 template <class T, int PT>
-hipError_t launch_d(const PagedAttendArgs& a, hipStream_t s) {
+hipError_t launch_d(const PagedAttendArgs& a, const ChunkPlan& c, hipStream_t s) {
   switch (a.p.d_h) {
-    case 64: return launch_one<T, PT, 64>(a, s);
-    case 128: return launch_one<T, PT, 128>(a, s);
-    case 256: return launch_one<T, PT, 256>(a, s);
+    case 64: return launch_one<T, PT, 64>(a, c, s);
+    case 128: return launch_one<T, PT, 128>(a, c, s);
+    case 256: return launch_one<T, PT, 256>(a, c, s);
     default: return hipErrorInvalidValue;
   }
 }
 template <class T>
-hipError_t launch_t(const PagedAttendArgs& a, int page_type, hipStream_t s) {
+hipError_t launch_t(const PagedAttendArgs& a, const ChunkPlan& c, int page_type, hipStream_t s) {
   switch (page_type) {
-    case kPages16: return launch_d<T, kPages16>(a, s);
-    case kPagesI8: return launch_d<T, kPagesI8>(a, s);
-    case kPagesE4M3: return launch_d<T, kPagesE4M3>(a, s);
+    case kPages16: return launch_d<T, kPages16>(a, c, s);
+    case kPagesI8: return launch_d<T, kPagesI8>(a, c, s);
+    case kPagesE4M3: return launch_d<T, kPagesE4M3>(a, c, s);
     default: return hipErrorInvalidValue;
   }
 }
 
 }  // namespace
 
-hipError_t launch_paged_chunk(const PagedAttendArgs& a, int dtype, int page_type, hipStream_t s) {
-  return dtype == 1 ? launch_t<BF16>(a, page_type, s) : launch_t<F16>(a, page_type, s);
+hipError_t launch_paged_chunk(const PagedAttendArgs& a, const ChunkPlan& c, int dtype, int page_type, hipStream_t s) {
+  return dtype == 1 ? launch_t<BF16>(a, c, page_type, s) : launch_t<F16>(a, c, page_type, s);
 }
 
 }  // namespace sparq
