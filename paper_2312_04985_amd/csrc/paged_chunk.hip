@@ -40,16 +40,18 @@ template <int DH> __device__ __forceinline__ int value_turn(int row) { return DH
 template <int DH> __device__ __forceinline__ int key_piece(int row, int piece) { return row * DH + ((piece ^ key_turn<DH>(row)) << 3); }
 template <int DH> __device__ __forceinline__ int value_piece(int row, int piece) { return row * DH + ((piece ^ value_turn<DH>(row)) << 3); }
 
-// 16 bytes per lane from memory into LDS at `to` + 16 lane, without a way through registers
-__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
-  typedef __attribute__((address_space(1))) const void gvoid;
+// 16 bytes per lane from memory (base + the lane's offset) into LDS at `to` + 16 lane, without a way through registers: the
+// instruction has no result but what tile_barrier waits for.  (The builtin for it makes every transposing read wait for all
+// such loads, those into the other buffer too: the prompt of 8192 took 820 us with it.)
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, void* to) {
   typedef __attribute__((address_space(3))) void lvoid;
-  __builtin_amdgcn_global_load_lds((gvoid*)from, (lvoid*)to, 16, 0, 0);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"((uint32_t)(uintptr_t)(lvoid*)to), "v"(off), "s"(base) : "memory");
 }
 
 // All of this wave's loads have arrived and its LDS accesses are done; then all waves' have.
 __device__ __forceinline__ void tile_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);                          // vmcnt(0) lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -62,11 +64,14 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
   constexpr int LOADS = 16 * PIECES / 64 / GW;                 // 16-bit pages: loads of 1 KB per wave, keys and values each
   constexpr int CL = PT == kPages16 ? 1 : (DH / 64 / GW > 0 ? DH / 64 / GW : 1);   // 8-bit pages: loads of 16 codes per lane
   static_assert(NW == 4 || (NW == 8 && DH >= 128), "whole loads");
-  __shared__ __align__(16) uint16_t Kt[2][kTile * DH], Vt[2][kTile * DH];
-  __shared__ __align__(16) float s_k[2][kTile], s_log[2][kTile], s_inv[2][kTile];   // 8-bit pages: scale of the key, log2 and inverse of the value's
-  __shared__ int64_t sum_w[NW];
-  __shared__ int s_begin[4];
-  __shared__ int flag;
+  // One object: of several, the compiler lets reads of one wait for loads into another.
+  struct Lds {
+    uint16_t Kt[2][kTile * DH], Vt[2][kTile * DH];
+    float s_k[2][kTile], s_log[2][kTile], s_inv[2][kTile];     // 8-bit pages: scale of the key, log2 and inverse of the value's
+    int64_t sum_w[NW];
+    int begin[4], found[NW], flag;
+  };
+  __shared__ __align__(16) Lds lds;
   const PagedArgs& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const bool packed = p.row_start != nullptr;
@@ -100,11 +105,11 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     if (r.err && me == 0 && lane == 0) atomicOr(p.err, r.err);
     mine += steps_of_unit(r);
   }
-  if (lane == 0) sum_w[wave] = mine;
+  if (lane == 0) lds.sum_w[wave] = mine;
   __syncthreads();
   int64_t before = 0, total = 0;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) { before += w < wave ? sum_w[w] : 0; total += sum_w[w]; }
+  for (int w = 0; w < NW; ++w) { before += w < wave ? lds.sum_w[w] : 0; total += lds.sum_w[w]; }
   before *= p.H_kv; total *= p.H_kv;
   const int64_t share = total < INT32_MAX - G ? (int64_t)divided((int)total + G - 1, by_G) : (total + G - 1) / G;
   const int64_t begin = (int64_t)me * share, end = begin + share < total ? begin + share : total;
@@ -130,15 +135,15 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
       for (int o = 1; o < kWave; o <<= 1) { const uint32_t x = __shfl_up(upto, o); if (lane >= o) upto += x; }
       const uint64_t past = __ballot((int64_t)upto > rest);
       if (past) {
-        if (lane == __builtin_ctzll(past)) { s_begin[0] = b; s_begin[1] = hk; s_begin[2] = k0 + lane; s_begin[3] = (int)(rest - (upto - cnt)); }
+        if (lane == __builtin_ctzll(past)) { lds.begin[0] = b; lds.begin[1] = hk; lds.begin[2] = k0 + lane; lds.begin[3] = (int)(rest - (upto - cnt)); }
         break;
       }
       rest -= __shfl(upto, 63);
     }
   }
   __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane(s_begin[0]), hk = __builtin_amdgcn_readfirstlane(s_begin[1]), tile = __builtin_amdgcn_readfirstlane(s_begin[2]),
-      skip = __builtin_amdgcn_readfirstlane(s_begin[3]);        // steps of the first row tile that are others'
+  int b = __builtin_amdgcn_readfirstlane(lds.begin[0]), hk = __builtin_amdgcn_readfirstlane(lds.begin[1]), tile = __builtin_amdgcn_readfirstlane(lds.begin[2]),
+      skip = __builtin_amdgcn_readfirstlane(lds.begin[3]);        // steps of the first row tile that are others'
 
   for (int64_t at = begin; at < end;) {
     const SeqRows r = rows_of(b);
@@ -181,24 +186,30 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     // ---- loads: a wave's part of a tile is 16 positions, which share a page ----
     const int p_begin = from + skip * kTile, p_end = from + (skip + todo) * kTile < to ? from + (skip + todo) * kTile : to;
     const int group = wave / GW, part = wave % GW;
+    // The pages of the next 64 tiles' parts, one per lane: a tile's loads do not wait for a page's.
+    int pages = 0, pages_from = 0;
+    auto part_at = [&](int p0) { const int x = p0 + group * 16; return x < to ? x : from; };   // (behind the last position: any row, its values are not used)
+    auto load_pages = [&](int p0) {
+      pages_from = p0;
+      pages = page_at(p, b, divided(part_at(lane < (to - p0) / kTile + 1 ? p0 + lane * kTile : p0), p.by_page));
+      if (pages < 0) { atomicOr(p.err, kErrBadPage); pages = 0; }
+    };
     auto place = [&](int p0) -> int64_t {
-      const int pos0 = p0 + group * 16, x = pos0 < to ? pos0 : from;   // (behind the last position: any row, its values are not used)
-      const int index = divided(x, p.by_page);
-      int page = page_at(p, b, index);
-      if (page < 0) { if (lane == 0) atomicOr(p.err, kErrBadPage); page = 0; }
-      return pool_row(p, page, hk, x - index * p.page_size);
+      if (p0 - pages_from >= kWave * kTile) load_pages(p0);
+      const int x = part_at(p0), index = divided(x, p.by_page);
+      return pool_row(p, __builtin_amdgcn_readlane(pages, (p0 - pages_from) / kTile), hk, x - index * p.page_size);
     };
     uint4 ck[CL], cv[CL];                                      // 8-bit pages: the next tile's codes and scales
     float csk = 0.0f, csv = 0.0f;
     auto issue = [&](int64_t row, int buf) {
       if constexpr (PT == kPages16) {
-        const uint16_t* kp = reinterpret_cast<const uint16_t*>(p.K) + row * DH;
-        const uint16_t* vp = reinterpret_cast<const uint16_t*>(p.V) + row * DH;
+        const char* kp = reinterpret_cast<const char*>(p.K) + row * (DH * 2);
+        const char* vp = reinterpret_cast<const char*>(p.V) + row * (DH * 2);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-          const int e = (part * LOADS + i) * 64 + lane, rr = group * 16 + e / PIECES, slot = e % PIECES, at8 = (group * 16 * PIECES + (part * LOADS + i) * 64) * 8;
-          load_to_lds(kp + (e / PIECES) * DH + (slot ^ key_turn<DH>(rr)) * 8, &Kt[buf][at8]);
-          load_to_lds(vp + (e / PIECES) * DH + (slot ^ value_turn<DH>(rr)) * 8, &Vt[buf][at8]);
+          const int first = (part * LOADS + i) * 64, e = first + lane, rr = group * 16 + e / PIECES, slot = e % PIECES, at8 = (group * 16 * PIECES + first) * 8;
+          load_to_lds(kp, (uint32_t)((e / PIECES) * (DH * 2) + (slot ^ key_turn<DH>(rr)) * 16), &lds.Kt[buf][at8]);
+          load_to_lds(vp, (uint32_t)((e / PIECES) * (DH * 2) + (slot ^ value_turn<DH>(rr)) * 16), &lds.Vt[buf][at8]);
         }
       } else {
         const uint8_t* kp = reinterpret_cast<const uint8_t*>(p.K) + row * DH;
@@ -222,31 +233,29 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 #pragma unroll
         for (int i = 0; i < CL; ++i) {
           const int e = (part * CL + i) * 64 + lane, rr = group * 16 + e / (DH / 16), piece = e % (DH / 16) * 2;
-          put(&Kt[buf][key_piece<DH>(rr, piece)], &Kt[buf][key_piece<DH>(rr, piece + 1)], ck[i], true);
-          put(&Vt[buf][value_piece<DH>(rr, piece)], &Vt[buf][value_piece<DH>(rr, piece + 1)], cv[i], p0 + rr < to);
+          put(&lds.Kt[buf][key_piece<DH>(rr, piece)], &lds.Kt[buf][key_piece<DH>(rr, piece + 1)], ck[i], true);
+          put(&lds.Vt[buf][value_piece<DH>(rr, piece)], &lds.Vt[buf][value_piece<DH>(rr, piece + 1)], cv[i], p0 + rr < to);
         }
         if (part == 0 && lane < 16) {
           const float v = value_scale(csv);
-          s_k[buf][group * 16 + lane] = csk;
-          s_log[buf][group * 16 + lane] = log2_normal(v);
-          s_inv[buf][group * 16 + lane] = 1.0f / v;
+          lds.s_k[buf][group * 16 + lane] = csk;
+          lds.s_log[buf][group * 16 + lane] = log2_normal(v);
+          lds.s_inv[buf][group * 16 + lane] = 1.0f / v;
         }
       }
     };
 
-    int64_t row_next = 0;
     if (p_begin < p_end) {
+      load_pages(p_begin);
       issue(place(p_begin), 0);
       settle(p_begin, 0);
-      row_next = place(p_begin + kTile);
     }
     for (int p0 = p_begin, buf = 0; p0 < p_end; p0 += kTile, buf ^= 1) {
       tile_barrier();                                          // this tile is there; nobody reads the other buffer
       const bool more = p0 + kTile < p_end;
-      if (more) issue(row_next, buf ^ 1);
-      row_next = place(p0 + 2 * kTile);
-      uint16_t* const kt = Kt[buf];
-      uint16_t* const vt = Vt[buf];
+      if (more) issue(place(p0 + kTile), buf ^ 1);
+      uint16_t* const kt = lds.Kt[buf];
+      uint16_t* const vt = lds.Vt[buf];
       if constexpr (PT == kPages16) {
         if (p0 + kTile > to) {                                 // values behind the last position: zeros
           for (int e = tid; e < (p0 + kTile - to) * PIECES; e += NTH) *reinterpret_cast<uint4*>(&vt[(to - p0) * DH + e * 8]) = make_uint4(0, 0, 0, 0);
@@ -260,12 +269,23 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
       f32x16 S[2];
       if (active) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e) S[i][e] = 0.0f;
+        // (the next four reads are on their way before these four products begin)
+        uint4 kf[2][4];
+        auto fetch = [&](int s) {
 #pragma unroll
-          for (int s = 0; s < DH / 16; ++s)
-            S[i] = mfma_32x32x16<E>(*reinterpret_cast<const uint4*>(&kt[key_piece<DH>(i * 32 + col, 2 * s + half)]), qf[s], S[i]);
+          for (int e = 0; e < 4; ++e) kf[s / 2 % 2][e] = *reinterpret_cast<const uint4*>(&kt[key_piece<DH>(e % 2 * 32 + col, 2 * (s + e / 2) + half)]);
+        };
+        fetch(0);
+#pragma unroll
+        for (int s = 0; s < DH / 16; s += 2) {
+          if (s + 2 < DH / 16) fetch(s + 2);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) S[e % 2] = mfma_32x32x16<E>(kf[s / 2 % 2][e], qf[s + e / 2], S[e % 2]);
+          __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (PT != kPages16) {
 #pragma unroll
@@ -273,7 +293,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const int j = 32 * i + 8 * (e / 4) + e % 4 + 4 * half;
-              S[i][e] = fmaf(S[i][e], s_k[buf][j] * c_row, s_log[buf][j]);
+              S[i][e] = fmaf(S[i][e], lds.s_k[buf][j] * c_row, lds.s_log[buf][j]);
             }
         }
         const bool masked = p0 < w_last.lo || p0 + kTile > w_first.hi;
@@ -319,7 +339,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const int j = 32 * i + 8 * (e / 4) + e % 4;
-              float inv = s_inv[buf][j + 4 * half];
+              float inv = lds.s_inv[buf][j + 4 * half];
               if (masked && at0 + j >= len) inv = 0.0f;        // (whatever the scale of a position that is not seen: 0 times it)
               l = fmaf(S[i][e], inv, l);
             }
@@ -332,8 +352,15 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
         if (p0 < wg_last.lo || p0 + kTile > wg_first.hi) {
           bool found = false;
           for (int e = tid; e < kTile * PIECES; e += NTH) found = found || has_special<T>(*reinterpret_cast<const uint4*>(&vt[e * 8]));
-          if (__syncthreads_or(found)) {
+          if (lane == 0) lds.found[wave] = 0;
+          if (found) lds.found[wave] = 1;                      // (the same word by the lanes that found some, behind the 0 of lane 0)
+          __syncthreads();
+          int any = 0;
+#pragma unroll
+          for (int w = 0; w < NW; ++w) any |= lds.found[w];
+          if (__builtin_amdgcn_readfirstlane(any)) {
             if (active)
+#pragma unroll 1
               for (int j = 0; j < kTile; ++j) {
                 if ((uint32_t)(p0 + j - lo) >= len) continue;
 #pragma unroll
@@ -355,18 +382,27 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 
       // ---- output ----
       if (active) {
-#pragma unroll
-        for (int sl = 0; sl < 4; ++sl) {
-          const int e0 = sl % 2 * 8;
-          const f32x16& w = S[sl / 2];
-          const uint4 pw = make_uint4(narrow2<E>(w[e0], w[e0 + 1]), narrow2<E>(w[e0 + 2], w[e0 + 3]), narrow2<E>(w[e0 + 4], w[e0 + 5]), narrow2<E>(w[e0 + 6], w[e0 + 7]));
+        uint4 vf[2][ND];                                       // the values of 16 positions and of the next 16
+        auto fetch = [&](int sl) {
           const int row = sl * 16 + 4 * half + (lane & 15) / 4;
 #pragma unroll
           for (int j = 0; j < ND; ++j) {
             const int piece = 4 * j + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), sub = (lane & 1) * 4;
             const uint2 v0 = lds_read_transposed(&vt[value_piece<DH>(row, piece) + sub]), v1 = lds_read_transposed(&vt[value_piece<DH>(row + 8, piece) + sub]);
-            O[j] = mfma_32x32x16<E>(make_uint4(v0.x, v0.y, v1.x, v1.y), pw, O[j]);
+            vf[sl % 2][j] = make_uint4(v0.x, v0.y, v1.x, v1.y);
           }
+        };
+        fetch(0);
+#pragma unroll
+        for (int sl = 0; sl < 4; ++sl) {
+          if (sl < 3) fetch(sl + 1);
+          const int e0 = sl % 2 * 8;
+          const f32x16& w = S[sl / 2];
+          const uint4 pw = make_uint4(narrow2<E>(w[e0], w[e0 + 1]), narrow2<E>(w[e0 + 2], w[e0 + 3]), narrow2<E>(w[e0 + 4], w[e0 + 5]), narrow2<E>(w[e0 + 6], w[e0 + 7]));
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < ND; ++j) O[j] = mfma_32x32x16<E>(vf[sl % 2][j], pw, O[j]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       if (more) settle(p0 + kTile, buf ^ 1);
@@ -385,26 +421,30 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 #pragma unroll
         for (int q = 0; q < 4; ++q) store_agent4(dst, (uint32_t)((j * 4 + q) * NTH + tid) * 16, make_float4(O[j][4 * q], O[j][4 * q + 1], O[j][4 * q + 2], O[j][4 * q + 3]));
       store_agent4(dst, (uint32_t)(ND * 4 * NTH + tid) * 16, make_float4(m_ref, l, 0.0f, 0.0f));
-      write = last_to_arrive(tickets + first_wg, last_wg - first_wg + 1, &flag);
+      write = last_to_arrive(tickets + first_wg, last_wg - first_wg + 1, &lds.flag);
       if (write) {                                             // in the order of the line, whoever is last
         m_ref = -INFINITY; l = 0.0f;
 #pragma unroll
         for (int j = 0; j < ND; ++j)
 #pragma unroll
           for (int i = 0; i < 16; ++i) O[j][i] = 0.0f;
+#pragma unroll 1
         for (int wg = first_wg; wg <= last_wg; ++wg) {
           const float* src = slot_of(wg);
           const float4 st = load_agent4(src, (uint32_t)(ND * 4 * NTH + tid) * 16);
-          float4 o[ND * 4];
-#pragma unroll
-          for (int i = 0; i < ND * 4; ++i) o[i] = load_agent4(src, (uint32_t)(i * NTH + tid) * 16);
           const float m_to = fmaxf(m_ref, st.x), f = weight_exp2(m_ref, m_to), g = weight_exp2(st.x, m_to);
           m_ref = m_to;
           l = l * f + st.y * g;
 #pragma unroll
-          for (int i = 0; i < ND * 4; ++i) {
-            O[i / 4][i % 4 * 4] = O[i / 4][i % 4 * 4] * f + o[i].x * g; O[i / 4][i % 4 * 4 + 1] = O[i / 4][i % 4 * 4 + 1] * f + o[i].y * g;
-            O[i / 4][i % 4 * 4 + 2] = O[i / 4][i % 4 * 4 + 2] * f + o[i].z * g; O[i / 4][i % 4 * 4 + 3] = O[i / 4][i % 4 * 4 + 3] * f + o[i].w * g;
+          for (int j = 0; j < ND; ++j) {
+            float4 o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[q] = load_agent4(src, (uint32_t)((j * 4 + q) * NTH + tid) * 16);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              O[j][4 * q] = O[j][4 * q] * f + o[q].x * g; O[j][4 * q + 1] = O[j][4 * q + 1] * f + o[q].y * g;
+              O[j][4 * q + 2] = O[j][4 * q + 2] * f + o[q].z * g; O[j][4 * q + 3] = O[j][4 * q + 3] * f + o[q].w * g;
+            }
           }
         }
       }
