@@ -21,6 +21,8 @@ namespace sparq {
 namespace {
 
 constexpr int kTile = 64;               // positions per tile
+// What a row tile costs besides its tiles of positions (queries, first loads, results), in tiles.
+constexpr int kStart = 4;
 constexpr int kWaves = chunk_rows / 32; // waves of a workgroup
 
 // c[m][n] += sum_k a[m][k] b[n][k] over 16 k: lane l holds a[l % 32], b[l % 32] at k = 8 (l / 32) .. + 7 and
@@ -79,12 +81,13 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
   // ---- this workgroup's part of the line ----
   auto rows_of = [&](int b) { return seq_rows(p.seq_lens[b], p.bound, p.n, p.n_per_seq, p.row_start, p.n_rows, b); };
   auto tiles_of = [&](const SeqRows& r) { const int M = r.n * a.group; return M <= a.skip_rows ? 0 : (M + ROWS - 1) / ROWS; };
-  // tiles of 64 positions that row tile k sees, from position `from` on (one at least: rows that see nothing are written too)
+  // The line is counted in tiles of 64 positions: those that row tile k sees, from position `from` on (one at least: rows that see
+  // nothing are written too), behind kStart that stand for its start and end.
   auto steps_of = [&](const SeqRows& r, int k, int& from, int& to) {
     const int M = r.n * a.group, m0 = k * ROWS, m1 = m0 + ROWS < M ? m0 + ROWS : M;
     from = seen_by(a, r, divided(m0, a.by_group)).lo & ~(kTile - 1);
     to = seen_by(a, r, divided(m1 - 1, a.by_group)).hi;
-    return to - from <= kTile ? 1 : (to - from + kTile - 1) / kTile;
+    return kStart + (to - from <= kTile ? 1 : (to - from + kTile - 1) / kTile);
   };
   auto steps_of_unit = [&](const SeqRows& r) -> int64_t {      // by all lanes of a wave together
     const int n_tiles = tiles_of(r);
@@ -157,6 +160,11 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     const int steps = steps_of(r, tile, from, to);
     const int todo = (int)(end - at < steps - skip ? end - at : steps - skip);
     const int64_t tile_at = at - skip;
+    const int k0 = skip > kStart ? skip - kStart : 0, k1 = skip + todo - kStart;   // its tiles of positions here
+    if (k1 <= k0) {                                            // (the start alone is no part of a row tile)
+      at += todo; skip = 0; ++tile;
+      continue;
+    }
 
     // ---- the lane's row ----
     const int M = r.n * a.group, m0 = tile * ROWS, m_w = m0 + wave * 32, m_last = M - 1;
@@ -184,7 +192,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     float m_ref = -INFINITY, l = 0.0f;
 
     // ---- loads: a wave's part of a tile is 16 positions, which share a page ----
-    const int p_begin = from + skip * kTile, p_end = from + (skip + todo) * kTile < to ? from + (skip + todo) * kTile : to;
+    const int p_begin = from + k0 * kTile, p_end = from + k1 * kTile < to ? from + k1 * kTile : to;
     const int group = wave / GW, part = wave % GW;
     // The pages of the next 64 tiles' parts, one per lane: a tile's loads do not wait for a page's.
     int pages = 0, pages_from = 0;
@@ -279,6 +287,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
           for (int e = 0; e < 4; ++e) kf[s / 2 % 2][e] = *reinterpret_cast<const uint4*>(&kt[key_piece<DH>(e % 2 * 32 + col, 2 * (s + e / 2) + half)]);
         };
         fetch(0);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int s = 0; s < DH / 16; s += 2) {
           if (s + 2 < DH / 16) fetch(s + 2);
@@ -287,6 +296,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
           for (int e = 0; e < 4; ++e) S[e % 2] = mfma_32x32x16<E>(kf[s / 2 % 2][e], qf[s + e / 2], S[e % 2]);
           __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
         if constexpr (PT != kPages16) {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
@@ -393,6 +403,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
           }
         };
         fetch(0);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int sl = 0; sl < 4; ++sl) {
           if (sl < 3) fetch(sl + 1);
@@ -404,6 +415,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
           for (int j = 0; j < ND; ++j) O[j] = mfma_32x32x16<E>(vf[sl % 2][j], pw, O[j]);
           __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
       }
       if (more) settle(p0 + kTile, buf ^ 1);
     }
@@ -411,8 +423,8 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     // ---- a row tile that several workgroups share: partial results in the order of registers ----
     const int64_t tile_end = tile_at + steps;
     bool write = true;
-    if (skip != 0 || todo != steps) {
-      const int first_wg = skip == 0 ? me : (int)(tile_at / share), last_wg = tile_end <= end ? me : (int)((tile_end - 1) / share);
+    if (k0 != 0 || k1 != steps - kStart) {
+      const int first_wg = k0 == 0 ? me : (int)((tile_at + kStart) / share), last_wg = tile_end <= end ? me : (int)((tile_end - 1) / share);
       constexpr int SLOT = NTH * (DH / 2 + 4);                 // floats: a lane's DH / 2 numerators, its maximum and its part of the denominator
       auto slot_of = [&](int wg) { return partials + ((size_t)wg * 2 + (wg == first_wg ? 1 : 0)) * SLOT; };
       float* dst = slot_of(me);
@@ -436,14 +448,15 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
           m_ref = m_to;
           l = l * f + st.y * g;
 #pragma unroll
-          for (int j = 0; j < ND; ++j) {
-            float4 o[4];
+          for (int j = 0; j < ND; j += 2) {
+            float4 o[8];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = load_agent4(src, (uint32_t)((j * 4 + q) * NTH + tid) * 16);
+            for (int q = 0; q < 8; ++q) o[q] = load_agent4(src, (uint32_t)((j * 4 + q) * NTH + tid) * 16);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              O[j][4 * q] = O[j][4 * q] * f + o[q].x * g; O[j][4 * q + 1] = O[j][4 * q + 1] * f + o[q].y * g;
-              O[j][4 * q + 2] = O[j][4 * q + 2] * f + o[q].z * g; O[j][4 * q + 3] = O[j][4 * q + 3] * f + o[q].w * g;
+            for (int q = 0; q < 8; ++q) {
+              f32x16& x = O[j + q / 4];
+              const int e = q % 4 * 4;
+              x[e] = x[e] * f + o[q].x * g; x[e + 1] = x[e + 1] * f + o[q].y * g; x[e + 2] = x[e + 2] * f + o[q].z * g; x[e + 3] = x[e + 3] * f + o[q].w * g;
             }
           }
         }
