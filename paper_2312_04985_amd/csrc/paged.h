@@ -96,7 +96,8 @@ constexpr int chunk_rows = 128;
 constexpr int chunk_per_cu(int d_h) { return d_h == 256 ? 1 : 2; }
 struct ChunkPlan {
   int workgroups;
-  float* partials;                                      // [workgroups][2][2 chunk_rows lanes][d_h / 2 + 4]
+  int tiles;                                            // row tiles per (sequence, KV head), each by a workgroup of its own; 0: equal parts of the work
+  float* partials;                                      // ... which leave [workgroups][2][2 chunk_rows lanes][d_h / 2 + 4] for each other
   int32_t* tickets;                                     // [workgroups], 0 between launches
 };
 

@@ -76,7 +76,15 @@ int tokens_workgroups(const sparq_paged_shape* s) {
   return (int)(units * 64 < most ? units * 64 : most);
 }
 
-// Workgroups of the second kernel: what runs at once, and no more than could have work (a row tile, and 4 tiles of positions of one).
+// Row tiles of the second kernel per (sequence, KV head) if a workgroup serves each, 0 if they are cut into equal parts of the work:
+// where the host cannot know how many there are, and where they are fewer than three quarters of the workgroups that run at once (measured in
+// paged_chunk.hip).
+int chunk_tiles(const sparq_paged_shape* s, int n, bool counted) {
+  const int64_t rows = (int64_t)n * (s->H / s->H_kv), tiles = (rows + chunk_rows - 1) / chunk_rows;
+  return !counted && tiles * s->B * s->H_kv * 4 >= (int64_t)3 * 256 * chunk_per_cu(s->d_h) ? (int)tiles : 0;
+}
+
+// Workgroups of the second kernel for equal parts: what runs at once, and no more than could have work (a row tile, and 4 tiles of positions of one).
 int chunk_workgroups(const sparq_paged_shape* s, int n) {
   const int64_t rows = (int64_t)n * (s->H / s->H_kv), bound = s->S_bound > 0 ? s->S_bound : (int64_t)s->max_pages * s->page_size;
   const int64_t tiles = (int64_t)s->B * s->H_kv * ((rows + chunk_rows - 1) / chunk_rows), most = 256 * chunk_per_cu(s->d_h);
@@ -178,7 +186,8 @@ int sparq_paged_attention(const sparq_paged_shape* shape, const sparq_paged_cach
   }
   a.skip_rows = plan.tokens_rows;
   if (e == hipSuccess && plan.chunk) {
-    const ChunkPlan c{chunk_workgroups(shape, rows->n), reinterpret_cast<float*>(static_cast<char*>(workspace) + kControlBytes),
+    const int tiles = chunk_tiles(shape, rows->n, rows->n_per_seq || rows->row_start);
+    const ChunkPlan c{tiles ? tiles * shape->B * shape->H_kv : chunk_workgroups(shape, rows->n), tiles, reinterpret_cast<float*>(static_cast<char*>(workspace) + kControlBytes),
                       reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kTicketOffset)};
     e = launch_paged_chunk(a, c, shape->dtype, shape->page_type, s);
   }

@@ -12,9 +12,14 @@
 // A value's scale goes into the exponent: w_j = 2^(x_j + log2 s_j - m) is what multiplies the codes, and w_j / s_j what
 // is summed.  Neither needs a rounding that 16-bit pages do not have.
 //
-// The work of the whole batch is one line of (sequence, KV head, row tile, tile of 64 positions) in order, cut into equal parts,
-// one per workgroup: chunks of different lengths, a causal mask's unequal row tiles and few rows over a long cache all load the
-// chip evenly.  A row tile that several workgroups share is put together by the last of them to finish.
+// Two ways to divide the work.  Where the host knows that there are row tiles enough, a workgroup serves one of them; the
+// dispatcher levels their sizes out, and the workgroups of a KV head, which read the same rows, run next to each other on one XCD.
+// Otherwise the work of the whole batch is one line of (sequence, KV head, row tile, tile of 64 positions) in order, cut into equal
+// parts, one per workgroup: chunks of different lengths and few rows over a long cache load the chip evenly as well.  A row tile
+// that several workgroups share is put together by the last of them to finish.
+// us, row tiles / the line (128 channels, f16; row tiles of all KV heads): 32 heads of 512 rows behind 8192 positions, 256 row tiles 216 / 194,
+// 384 278 / 311, 512 318 / 321, 640 474 / 515, 768 514 / 592, 1024 642 / 732, 1536 914 / 1117; prompts of 1024, 2048, 4096 and 8192, 256 35.5 / 40,
+// 512 75.6 / 71, 1024 212 / 215, 2048 622 / 680; 8 KV heads of 4 heads, prompts of 4096, 1024 162 / 180.
 #include "paged_core.h"
 
 namespace sparq {
@@ -59,7 +64,7 @@ __device__ __forceinline__ void tile_barrier() {
 }
 
 template <class T, int PT, int DH>
-__global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(const PagedAttendArgs a, const int G, const Divider by_G, float* partials, int32_t* tickets) {
+__global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(const PagedAttendArgs a, const ChunkPlan plan, const Divider by_G) {
   using E = Product<T, PT>;
   constexpr int NW = kWaves, NTH = NW * 64, ROWS = NW * 32, PIECES = DH / 8, ND = DH / 32;
   constexpr int GW = NW / 4;                                   // waves that load one group of 16 positions
@@ -77,8 +82,9 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
   const PagedArgs& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const bool packed = p.row_start != nullptr;
+  const int G = plan.workgroups;
+  float* const partials = plan.partials;
 
-  // ---- this workgroup's part of the line ----
   auto rows_of = [&](int b) { return seq_rows(p.seq_lens[b], p.bound, p.n, p.n_per_seq, p.row_start, p.n_rows, b); };
   auto tiles_of = [&](const SeqRows& r) { const int M = r.n * a.group; return M <= a.skip_rows ? 0 : (M + ROWS - 1) / ROWS; };
   // The line is counted in tiles of 64 positions: those that row tile k sees, from position `from` on (one at least: rows that see
@@ -98,53 +104,70 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o);
     return sum;
   };
-  // Consecutive parts of the line share rows of the cache; so that they share an L2 too, each of the 8 XCDs, which workgroups are dealt
-  // to round-robin, takes an eighth of the line.
-  const int me = G % 8 == 0 ? (int)(blockIdx.x % 8) * (G / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
-  const int per = (p.B + NW - 1) / NW, b_first = wave * per, b_last = b_first + per < p.B ? b_first + per : p.B;
-  int64_t mine = 0;
-  for (int b = b_first; b < b_last; ++b) {
-    const SeqRows r = rows_of(b);
-    if (r.err && me == 0 && lane == 0) atomicOr(p.err, r.err);
-    mine += steps_of_unit(r);
-  }
-  if (lane == 0) lds.sum_w[wave] = mine;
-  __syncthreads();
-  int64_t before = 0, total = 0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) { before += w < wave ? lds.sum_w[w] : 0; total += lds.sum_w[w]; }
-  before *= p.H_kv; total *= p.H_kv;
-  const int64_t share = total < INT32_MAX - G ? (int64_t)divided((int)total + G - 1, by_G) : (total + G - 1) / G;
-  const int64_t begin = (int64_t)me * share, end = begin + share < total ? begin + share : total;
-  if (begin >= end) return;
-  if (before <= begin && begin < before + mine * p.H_kv) {     // one wave
-    int64_t at = before, c = 1;
-    int b = b_first;
-    for (; b < b_last; ++b) {
-      c = steps_of_unit(rows_of(b));
-      if (begin < at + c * p.H_kv || b == b_last - 1) break;
-      at += c * p.H_kv;
+  // ---- this workgroup's part: [begin, end) of the line, or one row tile whole ----
+  int me = blockIdx.x;
+  int64_t share = 1, begin = 0, end = 0;
+  if (plan.tiles) {
+    // Workgroups are dealt round-robin to the 8 XCDs: eight (sequence, KV head) units at a time, the last row tiles, which see most, first.
+    const int units = p.B * p.H_kv, eight = blockIdx.x / (8 * plan.tiles), in_eight = blockIdx.x - eight * 8 * plan.tiles;
+    const int width = units - eight * 8 < 8 ? units - eight * 8 : 8, up = in_eight / width, unit = eight * 8 + in_eight - up * width;
+    const int b0 = divided(unit, p.by_H_kv), k = plan.tiles - 1 - up;
+    const SeqRows r = rows_of(b0);
+    if (r.err && k == 0 && unit == b0 * p.H_kv && tid == 0) atomicOr(p.err, r.err);
+    if (k >= tiles_of(r)) return;
+    int from, to;
+    end = steps_of(r, k, from, to);
+    if (tid == 0) { lds.begin[0] = b0; lds.begin[1] = unit - b0 * p.H_kv; lds.begin[2] = k; lds.begin[3] = 0; }
+    __syncthreads();
+  } else {
+    // Consecutive parts of the line share rows of the cache; so that they share an L2 too, each XCD takes an eighth of the line.
+    if (G % 8 == 0) me = (int)(blockIdx.x % 8) * (G / 8) + (int)blockIdx.x / 8;
+    const int per = (p.B + NW - 1) / NW, b_first = wave * per, b_last = b_first + per < p.B ? b_first + per : p.B;
+    int64_t mine = 0;
+    for (int b = b_first; b < b_last; ++b) {
+      const SeqRows r = rows_of(b);
+      if (r.err && me == 0 && lane == 0) atomicOr(p.err, r.err);
+      mine += steps_of_unit(r);
     }
-    const int64_t off = begin - at;
-    const int hk = (int)(off / (c > 0 ? c : 1));
-    int64_t rest = off - hk * c;
-    const SeqRows r = rows_of(b);
-    const int n_tiles = tiles_of(r);
-    for (int k0 = 0; k0 < n_tiles; k0 += kWave) {
-      int from, to;
-      const uint32_t cnt = k0 + lane < n_tiles ? (uint32_t)steps_of(r, k0 + lane, from, to) : 0u;
-      uint32_t upto = cnt;
+    if (lane == 0) lds.sum_w[wave] = mine;
+    __syncthreads();
+    int64_t before = 0, total = 0;
 #pragma unroll
-      for (int o = 1; o < kWave; o <<= 1) { const uint32_t x = __shfl_up(upto, o); if (lane >= o) upto += x; }
-      const uint64_t past = __ballot((int64_t)upto > rest);
-      if (past) {
-        if (lane == __builtin_ctzll(past)) { lds.begin[0] = b; lds.begin[1] = hk; lds.begin[2] = k0 + lane; lds.begin[3] = (int)(rest - (upto - cnt)); }
-        break;
+    for (int w = 0; w < NW; ++w) { before += w < wave ? lds.sum_w[w] : 0; total += lds.sum_w[w]; }
+    before *= p.H_kv; total *= p.H_kv;
+    share = total < INT32_MAX - G ? (int64_t)divided((int)total + G - 1, by_G) : (total + G - 1) / G;
+    begin = (int64_t)me * share;
+    end = begin + share < total ? begin + share : total;
+    if (begin >= end) return;
+    if (before <= begin && begin < before + mine * p.H_kv) {     // one wave
+      int64_t at = before, c = 1;
+      int b = b_first;
+      for (; b < b_last; ++b) {
+        c = steps_of_unit(rows_of(b));
+        if (begin < at + c * p.H_kv || b == b_last - 1) break;
+        at += c * p.H_kv;
       }
-      rest -= __shfl(upto, 63);
+      const int64_t off = begin - at;
+      const int hk = (int)(off / (c > 0 ? c : 1));
+      int64_t rest = off - hk * c;
+      const SeqRows r = rows_of(b);
+      const int n_tiles = tiles_of(r);
+      for (int k0 = 0; k0 < n_tiles; k0 += kWave) {
+        int from, to;
+        const uint32_t cnt = k0 + lane < n_tiles ? (uint32_t)steps_of(r, k0 + lane, from, to) : 0u;
+        uint32_t upto = cnt;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) { const uint32_t x = __shfl_up(upto, o); if (lane >= o) upto += x; }
+        const uint64_t past = __ballot((int64_t)upto > rest);
+        if (past) {
+          if (lane == __builtin_ctzll(past)) { lds.begin[0] = b; lds.begin[1] = hk; lds.begin[2] = k0 + lane; lds.begin[3] = (int)(rest - (upto - cnt)); }
+          break;
+        }
+        rest -= __shfl(upto, 63);
+      }
     }
+    __syncthreads();
   }
-  __syncthreads();
   int b = __builtin_amdgcn_readfirstlane(lds.begin[0]), hk = __builtin_amdgcn_readfirstlane(lds.begin[1]), tile = __builtin_amdgcn_readfirstlane(lds.begin[2]),
       skip = __builtin_amdgcn_readfirstlane(lds.begin[3]);        // steps of the first row tile that are others'
 
@@ -433,7 +456,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 #pragma unroll
         for (int q = 0; q < 4; ++q) store_agent4(dst, (uint32_t)((j * 4 + q) * NTH + tid) * 16, make_float4(O[j][4 * q], O[j][4 * q + 1], O[j][4 * q + 2], O[j][4 * q + 3]));
       store_agent4(dst, (uint32_t)(ND * 4 * NTH + tid) * 16, make_float4(m_ref, l, 0.0f, 0.0f));
-      write = last_to_arrive(tickets + first_wg, last_wg - first_wg + 1, &lds.flag);
+      write = last_to_arrive(plan.tickets + first_wg, last_wg - first_wg + 1, &lds.flag);
       if (write) {                                             // in the order of the line, whoever is last
         m_ref = -INFINITY; l = 0.0f;
 #pragma unroll
@@ -489,7 +512,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 
 template <class T, int PT, int DH>
 hipError_t launch_one(const PagedAttendArgs& a, const ChunkPlan& c, hipStream_t s) {
-  hipLaunchKernelGGL((paged_chunk<T, PT, DH>), dim3(c.workgroups), dim3(kWaves * 64), 0, s, a, c.workgroups, make_divider(c.workgroups), c.partials, c.tickets);
+  hipLaunchKernelGGL((paged_chunk<T, PT, DH>), dim3(c.workgroups), dim3(kWaves * 64), 0, s, a, c, make_divider(c.workgroups));
   return hipGetLastError();
 }
 template <class T, int PT>

@@ -241,3 +241,19 @@ def test_broadcast_queries():
         out = torch.empty((2, 6, n, 64), dtype=torch.float16, device="cuda")
         built.c.attend(x, out=out)
         P.check_attention(built, q.expand(2, n, 6, 64), out.transpose(1, 2), [n, n])
+
+
+@pytest.mark.parametrize("d_h,b,h_kv,g,n,dtype,pages", [
+    (128, 43, 9, 1, 40, "f16", "16"),          # one row tile per KV head, not a multiple of eight of them
+    (64, 8, 8, 3, 390, "bf16", "i8"),          # ten each, the last of them not full
+    (256, 10, 10, 2, 140, "bf16", "e4m3"),
+])
+def test_a_workgroup_for_every_row_tile(d_h, b, h_kv, g, n, dtype, pages):
+    """The same number of rows everywhere, so many that no row tile is divided; lengths all different, one sequence of fewer positions than rows."""
+    lens = [n + (i * 37) % 211 for i in range(b)]
+    lens[1], lens[2] = n // 2, 0
+    built = P.Built(lens, h_kv * g, h_kv, d_h, dtype, pages, 16, 97).fill()
+    q = built.queries(n)
+    out, lse = attend(built, q)
+    P.check_attention(built, q, out, [n] * b, lse)
+    assert built.c.error_flags() == 0
