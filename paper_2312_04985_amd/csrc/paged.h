@@ -87,8 +87,8 @@ struct TokensPlan {
 };
 // The most rows that a workgroup's registers hold next to the positions in flight.
 constexpr int tokens_rows(int d_h) { return d_h == 64 ? 64 : (d_h == 128 ? 32 : 16); }
-// Workgroups per CU: the 32 KB that a wave has in flight at 256 channels of 16 bits leave room for one.
-constexpr int tokens_per_cu(int d_h, int page_type) { return d_h == 256 && page_type == kPages16 ? 1 : 2; }
+// Workgroups per CU by what they are built for: with 4096 sums a wave's registers are those of two.
+constexpr int tokens_per_cu(int d_h, int tile_rows) { return d_h * tile_rows >= 4096 ? 1 : 2; }
 constexpr int kTokensWorkgroups = 512;                  // at most
 
 // Many rows per (sequence, KV head): row tiles of chunk_rows rows.

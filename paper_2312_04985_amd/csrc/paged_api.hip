@@ -71,8 +71,8 @@ AttendPlan attend_plan(const sparq_paged_shape* s, int n, bool counted) {
 int tokens_tile(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
 
 // Workgroups of the first kernel: what runs at once, and no more than 64 for a unit, whose last one puts their results together.
-int tokens_workgroups(const sparq_paged_shape* s) {
-  const int64_t units = (int64_t)s->B * s->H_kv, most = 256 * tokens_per_cu(s->d_h, s->page_type);
+int tokens_workgroups(const sparq_paged_shape* s, int tile) {
+  const int64_t units = (int64_t)s->B * s->H_kv, most = 256 * tokens_per_cu(s->d_h, tile);
   return (int)(units * 64 < most ? units * 64 : most);
 }
 
@@ -93,7 +93,14 @@ int chunk_workgroups(const sparq_paged_shape* s, int n) {
 }
 
 // Scratch behind the control block; the two kernels of a call follow each other and share it.
-size_t tokens_scratch(const sparq_paged_shape* s, int rows) { return (size_t)tokens_workgroups(s) * 2 * tokens_tile(rows) * (s->d_h + 4) * sizeof(float); }
+size_t tokens_scratch(const sparq_paged_shape* s, int rows) {
+  size_t most = 0;
+  for (int tile = 16; tile <= tokens_tile(rows); tile *= 2) {
+    const size_t need = (size_t)tokens_workgroups(s, tile) * 2 * tile * (s->d_h + 4) * sizeof(float);
+    most = need > most ? need : most;
+  }
+  return most;
+}
 size_t chunk_scratch(const sparq_paged_shape* s, int n) { return (size_t)chunk_workgroups(s, n) * 2 * (2 * chunk_rows) * (s->d_h / 2 + 4) * sizeof(float); }
 
 // (calls of fewer rows than n need no more: they have at most as many rows per KV head, and row tiles, as are counted here)
@@ -180,7 +187,7 @@ int sparq_paged_attention(const sparq_paged_shape* shape, const sparq_paged_cach
   const AttendPlan plan = attend_plan(shape, rows->n, rows->n_per_seq || rows->row_start);
   hipError_t e = hipSuccess;
   if (plan.tokens_rows) {
-    const TokensPlan t{tokens_workgroups(shape), plan.tokens_rows, reinterpret_cast<float*>(static_cast<char*>(workspace) + kControlBytes),
+    const TokensPlan t{tokens_workgroups(shape, tokens_tile(plan.tokens_rows)), plan.tokens_rows, reinterpret_cast<float*>(static_cast<char*>(workspace) + kControlBytes),
                        reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kTicketOffset)};
     e = launch_paged_tokens(a, t, shape->dtype, shape->page_type, s);
   }

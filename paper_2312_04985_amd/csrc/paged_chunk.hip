@@ -80,11 +80,12 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
   };
   __shared__ __align__(16) Lds lds;
   const PagedArgs& p = a.p;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+  const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const bool packed = p.row_start != nullptr;
   const int G = plan.workgroups;
   float* const partials = plan.partials;
 
+  const int lane0 = thread & 63;
   auto rows_of = [&](int b) { return seq_rows(p.seq_lens[b], p.bound, p.n, p.n_per_seq, p.row_start, p.n_rows, b); };
   auto tiles_of = [&](const SeqRows& r) { const int M = r.n * a.group; return M <= a.skip_rows ? 0 : (M + ROWS - 1) / ROWS; };
   // The line is counted in tiles of 64 positions: those that row tile k sees, from position `from` on (one at least: rows that see
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     const int n_tiles = tiles_of(r);
     int64_t sum = 0;
     int from, to;
-    for (int k = lane; k < n_tiles; k += kWave) sum += steps_of(r, k, from, to);
+    for (int k = lane0; k < n_tiles; k += kWave) sum += steps_of(r, k, from, to);
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o);
     return sum;
@@ -113,11 +114,11 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     const int width = units - eight * 8 < 8 ? units - eight * 8 : 8, up = in_eight / width, unit = eight * 8 + in_eight - up * width;
     const int b0 = divided(unit, p.by_H_kv), k = plan.tiles - 1 - up;
     const SeqRows r = rows_of(b0);
-    if (r.err && k == 0 && unit == b0 * p.H_kv && tid == 0) atomicOr(p.err, r.err);
+    if (r.err && k == 0 && unit == b0 * p.H_kv && thread == 0) atomicOr(p.err, r.err);
     if (k >= tiles_of(r)) return;
     int from, to;
     end = steps_of(r, k, from, to);
-    if (tid == 0) { lds.begin[0] = b0; lds.begin[1] = unit - b0 * p.H_kv; lds.begin[2] = k; lds.begin[3] = 0; }
+    if (thread == 0) { lds.begin[0] = b0; lds.begin[1] = unit - b0 * p.H_kv; lds.begin[2] = k; lds.begin[3] = 0; }
     __syncthreads();
   } else {
     // Consecutive parts of the line share rows of the cache; so that they share an L2 too, each XCD takes an eighth of the line.
@@ -126,10 +127,10 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     int64_t mine = 0;
     for (int b = b_first; b < b_last; ++b) {
       const SeqRows r = rows_of(b);
-      if (r.err && me == 0 && lane == 0) atomicOr(p.err, r.err);
+      if (r.err && me == 0 && lane0 == 0) atomicOr(p.err, r.err);
       mine += steps_of_unit(r);
     }
-    if (lane == 0) lds.sum_w[wave] = mine;
+    if (lane0 == 0) lds.sum_w[wave] = mine;
     __syncthreads();
     int64_t before = 0, total = 0;
 #pragma unroll
@@ -154,13 +155,13 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
       const int n_tiles = tiles_of(r);
       for (int k0 = 0; k0 < n_tiles; k0 += kWave) {
         int from, to;
-        const uint32_t cnt = k0 + lane < n_tiles ? (uint32_t)steps_of(r, k0 + lane, from, to) : 0u;
+        const uint32_t cnt = k0 + lane0 < n_tiles ? (uint32_t)steps_of(r, k0 + lane0, from, to) : 0u;
         uint32_t upto = cnt;
 #pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) { const uint32_t x = __shfl_up(upto, o); if (lane >= o) upto += x; }
+        for (int o = 1; o < kWave; o <<= 1) { const uint32_t x = __shfl_up(upto, o); if (lane0 >= o) upto += x; }
         const uint64_t past = __ballot((int64_t)upto > rest);
         if (past) {
-          if (lane == __builtin_ctzll(past)) { lds.begin[0] = b; lds.begin[1] = hk; lds.begin[2] = k0 + lane; lds.begin[3] = (int)(rest - (upto - cnt)); }
+          if (lane0 == __builtin_ctzll(past)) { lds.begin[0] = b; lds.begin[1] = hk; lds.begin[2] = k0 + lane0; lds.begin[3] = (int)(rest - (upto - cnt)); }
           break;
         }
         rest -= __shfl(upto, 63);
@@ -172,6 +173,9 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
       skip = __builtin_amdgcn_readfirstlane(lds.begin[3]);        // steps of the first row tile that are others'
 
   for (int64_t at = begin; at < end;) {
+    int tid = thread;
+    asm volatile("" : "+v"(tid));                              // (what follows from it is not to be kept in registers from one row tile to the next)
+    const int lane = tid & 63, col = lane & 31, half = lane >> 5;
     const SeqRows r = rows_of(b);
     const int n_tiles = tiles_of(r);
     if (tile >= n_tiles) {                                     // the next KV head or sequence (one with rows follows: at < end <= total)

@@ -42,8 +42,11 @@ template <int KL, int PT> struct Stage {
   float4 sk[2], sv[2];
 };
 
+// n / d for results that fit an int (64-bit divisions are long)
+__device__ __forceinline__ int quotient(int64_t n, int64_t d) { return n <= UINT32_MAX && d <= UINT32_MAX ? (int)((uint32_t)n / (uint32_t)d) : (int)(n / d); }
+
 template <class T, int PT, int DH, int NT>
-__global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const PagedAttendArgs a, const int max_rows, const int G, const Divider by_G, float* partials, int32_t* tickets) {
+__global__ __launch_bounds__(TT, tokens_per_cu(DH, 16 * NT)) void paged_tokens(const PagedAttendArgs a, const int max_rows, const int G, const Divider by_G, float* partials, int32_t* tickets) {
   using E = Product<T, PT>;
   using Geo = TokensGeometry<T, PT, DH, NT>;
   constexpr int ROWS = Geo::ROWS, KK = Geo::KK, KL = Geo::KL, STRIDE = Geo::STRIDE, NJ = DH / 16;
@@ -52,7 +55,7 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
   __shared__ int s_begin[4];
   __shared__ int flag;
   const PagedArgs& p = a.p;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
+  const int thread = threadIdx.x;
   const bool packed = p.row_start != nullptr;
 
   // ---- this workgroup's part of the line ----
@@ -71,20 +74,21 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
     range_of(r, from, to);
     return to - from <= kRun ? 1 : (to - from + kRun - 1) / kRun;
   };
-  const int per = (p.B + TT - 1) / TT, b_first = tid * per, b_last = b_first + per < p.B ? b_first + per : p.B;
+  const int lane0 = thread & 63, wave0 = thread >> 6;
+  const int per = (p.B + TT - 1) / TT, b_first = thread * per, b_last = b_first + per < p.B ? b_first + per : p.B;
   int64_t mine = 0;
   for (int b = b_first; b < b_last; ++b) mine += runs_of(b);
   int64_t upto = mine;                                             // inclusive prefix sum over the wave
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
     const int64_t x = __shfl_up(upto, o);
-    if (lane >= o) upto += x;
+    if (lane0 >= o) upto += x;
   }
-  if (lane == 63) sum_w[wave] = upto;
+  if (lane0 == 63) sum_w[wave0] = upto;
   __syncthreads();
   int64_t before = 0, total = 0;
 #pragma unroll
-  for (int w = 0; w < TW; ++w) { before += w < wave ? sum_w[w] : 0; total += sum_w[w]; }
+  for (int w = 0; w < TW; ++w) { before += w < wave0 ? sum_w[w] : 0; total += sum_w[w]; }
   before += upto - mine;
   total *= p.H_kv;
   const int64_t share = total < INT32_MAX - G ? (int64_t)divided((int)total + G - 1, by_G) : (total + G - 1) / G;
@@ -98,16 +102,19 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
       if (begin < at + c) break;
       at += c;
     }
-    const int runs = runs_of(b), c = runs > 0 ? runs : 1;
+    const int runs = per == 1 ? (int)mine : runs_of(b), c = runs > 0 ? runs : 1;
     const int64_t off = begin - at;
     s_begin[0] = b;
-    s_begin[1] = (int)(off / c);                                   // KV head
-    s_begin[2] = (int)(off % c);                                   // run
+    s_begin[1] = quotient(off, c);                                 // KV head
+    s_begin[2] = (int)(off - (int64_t)s_begin[1] * c);             // run
   }
   __syncthreads();
   int b = __builtin_amdgcn_readfirstlane(s_begin[0]), hk = __builtin_amdgcn_readfirstlane(s_begin[1]), run = __builtin_amdgcn_readfirstlane(s_begin[2]);
 
   for (int64_t at = begin; at < end;) {
+    int tid = thread;
+    asm volatile("" : "+v"(tid));                                  // (what follows from it is not to be kept in registers from one unit to the next: 75 of them)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
     const int runs = runs_of(b);
     if (runs == 0) {                                               // (a later sequence has runs: at < end <= total)
       if (++b >= p.B) return;
@@ -119,6 +126,49 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
     const int todo = (int)(end - at < runs - run ? end - at : runs - run);
     const int64_t unit_at = at - run;                              // of the unit's first run
     const int M = r.n * a.group;
+
+    const int lo_last = seen_by(a, r, r.n - 1).lo, hi_first = seen_by(a, r, 0).hi;
+    uint16_t* Vt = reinterpret_cast<uint16_t*>(lds) + wave * (kPos * DH);
+
+    using St = Stage<KL, PT>;
+    // The pages of the wave's next 32 turns, two groups of 16 positions each, one per lane: a turn's loads do not wait for a page's.
+    int pages = 0, pages_from = 0;
+    auto group_at = [&](int pos) { return pos < to ? pos : from; };   // (behind the last position: any row, its values are not used)
+    auto load_pages = [&](int p0) {
+      pages_from = p0;
+      const int turn = lane / 2 < (to - p0) / kRun + 1 ? lane / 2 : 0;
+      pages = page_at(p, b, divided(group_at(p0 + turn * kRun + lane % 2 * 16), p.by_page));
+      if (pages < 0) { atomicOr(p.err, kErrBadPage); pages = 0; }
+    };
+    auto place = [&](int p0, int i) -> int64_t {                   // row in the pool of a group of 16 positions
+      const int x = group_at(p0 + 16 * i), index = divided(x, p.by_page);
+      return pool_row(p, __builtin_amdgcn_readlane(pages, (p0 - pages_from) / kRun * 2 + i), hk, x - index * p.page_size);
+    };
+    auto load = [&](St& s, int p0) {
+      if (p0 - pages_from >= 32 * kRun) load_pages(p0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int64_t row = place(p0, i);
+        const char* kp = reinterpret_cast<const char*>(p.K) + row * (DH * Geo::EB) + (col * DH * Geo::EB + quarter * 16);
+        const char* vp = reinterpret_cast<const char*>(p.V) + row * (DH * Geo::EB) + lane * 16;
+#pragma unroll
+        for (int e = 0; e < KL; ++e) s.k[i][e] = load16(kp + e * 64);
+#pragma unroll
+        for (int e = 0; e < KL; ++e) s.v[i][e] = load16(vp + e * 1024);
+        if constexpr (PT != kPages16) {
+          s.sk[i] = *reinterpret_cast<const float4*>(p.K_scale + row + 4 * quarter);
+          s.sv[i] = *reinterpret_cast<const float4*>(p.V_scale + row + 4 * quarter);
+        }
+      }
+    };
+    const int p1 = from + (run + todo) * kRun < to ? from + (run + todo) * kRun : to;
+    St s;
+    int p0 = from + run * kRun + wave * kPos;
+    bool more = p0 < p1;
+    if (more) {
+      load_pages(p0);
+      load(s, p0);
+    }
 
     // ---- the lane's rows ----
     uint4 qf[NT][KK];
@@ -142,55 +192,19 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
 #pragma unroll
       for (int j = 0; j < NJ; ++j) O[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    const int lo_last = seen_by(a, r, r.n - 1).lo, hi_first = seen_by(a, r, 0).hi;
-    uint16_t* Vt = reinterpret_cast<uint16_t*>(lds) + wave * (kPos * DH);
-
-    using St = Stage<KL, PT>;
-    auto place = [&](int pos) -> int64_t {                         // row in the pool of a group of 16 positions
-      const int x = pos < to ? pos : from;
-      const int index = divided(x, p.by_page);
-      int page = page_at(p, b, index);
-      if (page < 0) { if (lane == 0) atomicOr(p.err, kErrBadPage); page = 0; }
-      return pool_row(p, page, hk, x - index * p.page_size);
-    };
-    auto load = [&](St& s, int p0) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int64_t row = place(p0 + 16 * i);
-        const char* kp = reinterpret_cast<const char*>(p.K) + row * (DH * Geo::EB) + (col * DH * Geo::EB + quarter * 16);
-        const char* vp = reinterpret_cast<const char*>(p.V) + row * (DH * Geo::EB) + lane * 16;
-#pragma unroll
-        for (int e = 0; e < KL; ++e) s.k[i][e] = load16(kp + e * 64);
-#pragma unroll
-        for (int e = 0; e < KL; ++e) s.v[i][e] = load16(vp + e * 1024);
-        if constexpr (PT != kPages16) {
-          s.sk[i] = *reinterpret_cast<const float4*>(p.K_scale + row + 4 * quarter);
-          s.sv[i] = *reinterpret_cast<const float4*>(p.V_scale + row + 4 * quarter);
-        }
-      }
-    };
     // ---- the positions: the next ones are loaded once this turn's are out of their registers ----
-    const int p1 = from + (run + todo) * kRun < to ? from + (run + todo) * kRun : to;
-    St s;
-    int p0 = from + run * kRun + wave * kPos;
-    bool more = p0 < p1;
-    if (more) load(s, p0);
     while (more) {
       more = p0 + kRun < p1;
-      // values into LDS; those outside [from, to), which no row sees, as zeros
-      const bool edge = p0 + kPos > to;
+      // values into LDS
       const bool masked = p0 < lo_last || p0 + kPos > hi_first;
-      bool special = false;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < KL; ++e) {
           constexpr int LPR = DH * Geo::EB / 16;                   // lanes per row
           const int at16 = e * 64 + lane, rr = 16 * i + at16 / LPR, piece = at16 % LPR;
-          uint4 v = s.v[i][e];
-          if (edge && p0 + rr >= to) v = make_uint4(0, 0, 0, 0);
+          const uint4& v = s.v[i][e];
           if constexpr (PT == kPages16) {
-            if (masked) special = special || has_special<T>(v);
             *reinterpret_cast<uint4*>(&Vt[piece_place<DH>(rr, piece)]) = v;
           } else {
             const uint2 x0 = codes_to_half<PT>(v.x), x1 = codes_to_half<PT>(v.y), x2 = codes_to_half<PT>(v.z), x3 = codes_to_half<PT>(v.w);
@@ -242,10 +256,19 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
             float x;
             if constexpr (PT == kPages16) x = S[nt][i][e] * c_row[nt];
             else { x = fmaf(S[nt][i][e], s_key[i][e] * c_row[nt], s_log[i][e]); inv[i][e] = s_inv[i][e]; }
-            if (masked && at + 16 * i + e >= len[nt]) { x = -INFINITY; inv[i][e] = 0.0f; }
             S[nt][i][e] = x;
-            mx = fmaxf(mx, x);
           }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (at + (16 * i + e) >= len[nt]) { S[nt][i][e] = -INFINITY; inv[i][e] = 0.0f; }   // (0: whatever the scale of a position that is not seen)
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, S[nt][i][e]);
         float x, y;
         lane_pair<16>(mx, x, y);
         lane_pair<32>(fmaxf(x, y), x, y);
@@ -269,27 +292,35 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
         w16[nt] = make_uint4(narrow2<E>(S[nt][0][0], S[nt][0][1]), narrow2<E>(S[nt][0][2], S[nt][0][3]), narrow2<E>(S[nt][1][0], S[nt][1][1]), narrow2<E>(S[nt][1][2], S[nt][1][3]));
       }
       wave_lds_fence();
-      if constexpr (PT == kPages16) {
-        if (masked && __ballot(special)) {
+      if (masked) {
+        // values behind the last position that some row sees: zeros
+        for (int e = (to - p0) * (DH / 8) + lane; e < kPos * (DH / 8); e += kWave) *reinterpret_cast<uint4*>(&Vt[e * 8]) = make_uint4(0, 0, 0, 0);
+        wave_lds_fence();
+        if constexpr (PT == kPages16) {
           // infinities and NaN among values that some rows do not see (a weight of 0 would make NaN of them): added to the
           // rows that see them, zeros in their places
-          for (int j = 0; j < kPos; ++j)
+          bool special = false;
+          for (int e = lane; e < kPos * (DH / 8); e += kWave) special = special || has_special<T>(*reinterpret_cast<const uint4*>(&Vt[e * 8]));
+          if (__ballot(special)) {
+#pragma unroll 1
+            for (int j = 0; j < kPos; ++j)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              if ((uint32_t)(p0 + j - lo[nt]) >= len[nt]) continue;
+              for (int nt = 0; nt < NT; ++nt) {
+                if ((uint32_t)(p0 + j - lo[nt]) >= len[nt]) continue;
 #pragma unroll
-              for (int jj = 0; jj < NJ; ++jj)
+                for (int jj = 0; jj < NJ; ++jj)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int d = 16 * jj + 4 * quarter + e;
-                  const float v = T::widen(Vt[piece_place<DH>(j, d / 8) + d % 8]);
-                  if (!(fabsf(v) < INFINITY)) O[nt][jj][e] += v;
-                }
-            }
-          wave_lds_fence();
-          for (int e = lane; e < kPos * DH; e += kWave)
-            if (!(fabsf(T::widen(Vt[e])) < INFINITY)) Vt[e] = 0;
-          wave_lds_fence();
+                  for (int e = 0; e < 4; ++e) {
+                    const int d = 16 * jj + 4 * quarter + e;
+                    const float v = T::widen(Vt[piece_place<DH>(j, d / 8) + d % 8]);
+                    if (!(fabsf(v) < INFINITY)) O[nt][jj][e] += v;
+                  }
+              }
+            wave_lds_fence();
+            for (int e = lane; e < kPos * DH; e += kWave)
+              if (!(fabsf(T::widen(Vt[e])) < INFINITY)) Vt[e] = 0;
+            wave_lds_fence();
+          }
         }
       }
       const int row = 4 * quarter + (lane & 15) / 4;
@@ -321,7 +352,7 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
     const int n_slots = M * (DH / 4);                              // 4 channels of a row each
     const int64_t unit_end = unit_at + runs;
     const bool whole = run == 0 && todo == runs;
-    const int first_wg = run == 0 ? (int)blockIdx.x : (int)(unit_at / share), last_wg = unit_end <= end ? (int)blockIdx.x : (int)((unit_end - 1) / share);
+    const int first_wg = run == 0 ? (int)blockIdx.x : quotient(unit_at, share), last_wg = unit_end <= end ? (int)blockIdx.x : quotient(unit_end - 1, share);
     auto slot_of = [&](int wg) { return partials + ((size_t)wg * 2 + (wg == first_wg ? 1 : 0)) * (ROWS * STRIDE); };
     auto finish = [&](int m, int c, const float4& y, float m_all, float l_all) {
       const int t = divided(m, a.by_group), head = hk * a.group + m - t * a.group;
@@ -353,30 +384,44 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, PT)) void paged_tokens(const 
       }
     }
     if (!whole && last_to_arrive(tickets + first_wg, last_wg - first_wg + 1, &flag)) {
-      // the parts of a unit in order, so that the sum does not depend on who comes last; four of them in flight
-      for (int slot = tid; slot < n_slots; slot += TT) {
+      // The parts of a unit in an order of their own, so that the sums do not depend on who comes last: threads that are left over by
+      // the slots share the parts of a slot, eight of them in flight each.
+      const int grps = n_slots < TT ? TT / n_slots : 1;
+      auto add = [](float4& y, float& m_all, float& l_all, const float4& o, float m_o, float l_o) {
+        const float m_new = fmaxf(m_all, m_o);
+        const float f = weight_exp2(m_all, m_new), g = weight_exp2(m_o, m_new);
+        l_all = l_all * f + l_o * g;
+        y.x = y.x * f + o.x * g; y.y = y.y * f + o.y * g; y.z = y.z * f + o.z * g; y.w = y.w * f + o.w * g;
+        m_all = m_new;
+      };
+      const int grp = grps > 1 ? tid / n_slots : 0;
+      float4* sum = reinterpret_cast<float4*>(lds);                // [TT] numerators, then [TT] (maximum, denominator)
+      for (int slot = grps > 1 ? tid - grp * n_slots : tid; slot < n_slots && grp < grps; slot += TT) {
         const int m = slot / (DH / 4), c = slot % (DH / 4) * 4;
         float m_all = -INFINITY, l_all = 0.0f;
         float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int wg = first_wg; wg <= last_wg; wg += 4) {
-          float4 o[4], st[4];
+        for (int wg = first_wg + grp; wg <= last_wg; wg += 8 * grps) {
+          float4 o[8], st[8];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float* src = slot_of(wg + i <= last_wg ? wg + i : wg);
-            o[i] = load_agent4(src, (uint32_t)(m * STRIDE + c) * 4);
-            st[i] = load_agent4(src, (uint32_t)(m * STRIDE + DH) * 4);
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t at_wg = (uint32_t)((wg + i * grps <= last_wg ? wg + i * grps : wg) - first_wg), off = (at_wg * 2 - (at_wg ? 1 : 0)) * (ROWS * STRIDE * 4);
+            o[i] = load_agent4(slot_of(first_wg), off + (uint32_t)(m * STRIDE + c) * 4);
+            st[i] = load_agent4(slot_of(first_wg), off + (uint32_t)(m * STRIDE + DH) * 4);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (wg + i > last_wg) continue;
-            const float m_new = fmaxf(m_all, st[i].x);
-            const float f = weight_exp2(m_all, m_new), g = weight_exp2(st[i].x, m_new);
-            l_all = l_all * f + st[i].y * g;
-            y.x = y.x * f + o[i].x * g; y.y = y.y * f + o[i].y * g; y.z = y.z * f + o[i].z * g; y.w = y.w * f + o[i].w * g;
-            m_all = m_new;
-          }
+          for (int i = 0; i < 8; ++i)
+            if (wg + i * grps <= last_wg) add(y, m_all, l_all, o[i], st[i].x, st[i].y);
         }
-        finish(m, c, y, m_all, l_all);
+        if (grps == 1) finish(m, c, y, m_all, l_all);
+        else { sum[tid] = y; sum[TT + tid] = make_float4(m_all, l_all, 0.0f, 0.0f); }
+      }
+      if (grps > 1) {
+        __syncthreads();
+        if (tid < n_slots) {
+          float4 y = sum[tid], st = sum[TT + tid];
+          for (int k = 1; k < grps; ++k) { const float4 s2 = sum[TT + k * n_slots + tid]; add(y, st.x, st.y, sum[k * n_slots + tid], s2.x, s2.y); }
+          finish(tid / (DH / 4), tid % (DH / 4) * 4, y, st.x, st.y);
+        }
       }
     }
     at += todo;
