@@ -332,7 +332,7 @@ typedef struct {
   const int32_t* row_start;  /* device [B + 1] or NULL; row_start[b + 1] - row_start[b] (0 .. n) is sequence b's count.  Not both. */
 } sparq_rows;
 
-typedef struct { int64_t seq, head, row; } sparq_strides;   /* elements, multiples of 8; channels are contiguous */
+typedef struct { int64_t seq, head, row; } sparq_strides;   /* elements, multiples of 8 (an extent of one has none); channels are contiguous */
 
 /* Bytes of device workspace that the paged calls need for calls of up to n rows per sequence (>= 64 KiB, initialised once with
  * sparq_workspace_init; a workspace for n rows serves calls of fewer).  One workspace serves one stream; graphs that may run at the same time need

@@ -143,8 +143,9 @@ def _dev(t: Optional[torch.Tensor], name: str, dtype=None) -> Optional[int]:
 
 
 def _stream(stream) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is None:      # the current device's current stream (a Stream object for it takes 2 us to make, a launch 4)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def make_shape(B, H, H_kv, S_max, d_h, r, k, dtype, flags=0, local_window=0, S_bound=0) -> SparqShape:
@@ -261,30 +262,29 @@ def _rows_dev(t: torch.Tensor, name: str, packed: bool):
     return t.data_ptr(), SparqStrides(0, s[1], s[0]) if packed else SparqStrides(s[0], s[1], s[2])
 
 
+def _pair_dev(a: torch.Tensor, b: torch.Tensor, what: str, packed: bool):
+    """The pointers of two tensors of rows that are laid out alike, and their strides."""
+    if a.stride() != b.stride() or a.shape != b.shape or a.dtype is not b.dtype or a.device != b.device:
+        raise ValueError(f"{what} must have the same type, shape, strides and device")
+    p, s = _rows_dev(a, what, packed)
+    return p, b.data_ptr(), s
+
+
 def sparq_paged_workspace_bytes(shape: SparqPagedShape, n: int) -> int:
     out = ctypes.c_size_t(0)
     _check("sparq_paged_workspace_bytes", load().sparq_paged_workspace_bytes(ctypes.byref(shape), int(n), ctypes.byref(out)))
     return int(out.value)
 
 
-def _same_strides(a: torch.Tensor, b: torch.Tensor, what: str) -> None:
-    if a.stride() != b.stride() or a.shape != b.shape:
-        raise ValueError(f"{what} must have the same shape and strides")
-
-
 def sparq_paged_append(shape, cache, rows, k_new, v_new, workspace, stream=None) -> None:
-    packed = rows.row_start is not None
-    _same_strides(k_new, v_new, "k_new and v_new")
-    (k, s), (v, _) = _rows_dev(k_new, "k_new", packed), _rows_dev(v_new, "v_new", packed)
+    k, v, s = _pair_dev(k_new, v_new, "k_new and v_new", rows.row_start is not None)
     _check("sparq_paged_append",
            load().sparq_paged_append(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), k, v, ctypes.byref(s),
                                      _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def sparq_paged_read(shape, cache, rows, first, K_out, V_out, workspace, stream=None) -> None:
-    packed = rows.row_start is not None
-    _same_strides(K_out, V_out, "K_out and V_out")
-    (k, s), (v, _) = _rows_dev(K_out, "K_out", packed), _rows_dev(V_out, "V_out", packed)
+    k, v, s = _pair_dev(K_out, V_out, "K_out and V_out", rows.row_start is not None)
     _check("sparq_paged_read",
            load().sparq_paged_read(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), _dev(first, "first", torch.int32), k, v,
                                    ctypes.byref(s), _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)))

@@ -37,14 +37,20 @@ int check_rows(const sparq_paged_shape* s, const sparq_rows* r) {
   return SPARQ_OK;
 }
 
+// The strides that a call steps along: those of extents of one are not looked at.
+RowStrides strides_of(const sparq_paged_shape* s, const sparq_rows* r, const sparq_strides* t, int heads) {
+  return RowStrides{!r->row_start && s->B > 1 ? t->seq : 0, heads > 1 ? t->head : 0, (r->row_start ? r->n_rows : r->n) > 1 ? t->row : 0};
+}
+
 // `written`: rows must not lie on top of each other
 int check_strides(const sparq_paged_shape* s, const sparq_rows* r, const sparq_strides* t, int heads, bool written) {
-  if (!t || t->seq < 0 || t->head < 0 || t->row < 0) return SPARQ_EINVAL;
-  if (t->seq % 8 || t->head % 8 || t->row % 8) return SPARQ_EINVAL;
+  if (!t) return SPARQ_EINVAL;
+  const RowStrides u = strides_of(s, r, t, heads);
+  if (u.seq < 0 || u.head < 0 || u.row < 0 || u.seq % 8 || u.head % 8 || u.row % 8) return SPARQ_EINVAL;
   if (!written) return SPARQ_OK;
-  if (!r->row_start && s->B > 1 && t->seq < s->d_h) return SPARQ_EINVAL;
-  if (heads > 1 && t->head < s->d_h) return SPARQ_EINVAL;
-  if ((r->row_start ? r->n_rows : r->n) > 1 && t->row < s->d_h) return SPARQ_EINVAL;
+  if (!r->row_start && s->B > 1 && u.seq < s->d_h) return SPARQ_EINVAL;
+  if (heads > 1 && u.head < s->d_h) return SPARQ_EINVAL;
+  if ((r->row_start ? r->n_rows : r->n) > 1 && u.row < s->d_h) return SPARQ_EINVAL;
   return SPARQ_OK;
 }
 
@@ -133,8 +139,6 @@ PagedArgs paged_args(const sparq_paged_shape* s, const sparq_paged_cache* c, con
   return p;
 }
 
-RowStrides strides_of(const sparq_strides* t) { return RowStrides{t->seq, t->head, t->row}; }
-
 int move_rows(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows, const int32_t* first, void* k, void* v,
               const sparq_strides* strides, void* workspace, size_t workspace_bytes, void* hip_stream, bool reads) {
   int rc = check_call(shape, cache, rows, workspace, workspace_bytes);
@@ -143,7 +147,7 @@ int move_rows(const sparq_paged_shape* shape, const sparq_paged_cache* cache, co
   if (rc != SPARQ_OK) return rc;
   PagedRowsArgs a{};
   a.p = paged_args(shape, cache, rows, workspace);
-  a.k = k; a.v = v; a.first = first; a.s = strides_of(strides);
+  a.k = k; a.v = v; a.first = first; a.s = strides_of(shape, rows, strides, shape->H_kv);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const hipError_t e = reads ? launch_paged_read(a, shape->dtype, shape->page_type, s) : launch_paged_append(a, shape->dtype, shape->page_type, s);
   return e == hipSuccess ? SPARQ_OK : SPARQ_ELAUNCH;
@@ -180,7 +184,7 @@ int sparq_paged_attention(const sparq_paged_shape* shape, const sparq_paged_cach
   if (rc != SPARQ_OK) return rc;
   PagedAttendArgs a{};
   a.p = paged_args(shape, cache, rows, workspace);
-  a.q = q; a.out = out; a.lse = lse_out; a.qs = strides_of(q_strides); a.os = strides_of(out_strides);
+  a.q = q; a.out = out; a.lse = lse_out; a.qs = strides_of(shape, rows, q_strides, shape->H); a.os = strides_of(shape, rows, out_strides, shape->H);
   a.window = shape->window; a.all = (shape->flags & SPARQ_FLAG_PAGED_ALL) != 0;
   a.group = shape->H / shape->H_kv; a.by_group = make_divider(a.group);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

@@ -4,7 +4,7 @@ Allocation and bookkeeping only (torch owns the memory); all work is done by lib
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple, Union
+from typing import Optional, Union
 
 import torch
 
@@ -60,7 +60,7 @@ class PagedCache:
                 raise ValueError("all buffers of a cache must live on one device")
         self.K, self.V, self.K_scale, self.V_scale, self.page_table, self.seq_lens = K, V, K_scale, V_scale, page_table, seq_lens
         self.B, self.H, self.H_kv, self.d_h, self.page_size, self.n_pages, self.max_pages = Bsz, H, H_kv, d_h, page_size, n_pages, max_pages
-        self.dtype, self.device = dtype, K.device
+        self.dtype, self.device, self._index = dtype, K.device, K.device.index
         self.cache = B.make_paged_cache(K, V, K_scale, V_scale, page_table, seq_lens)
         self.shape = B.make_paged_shape(Bsz, H, H_kv, d_h, page_size, n_pages, max_pages, dtype, PAGE_TYPES[self.pages],
                                         0 if causal else B.SPARQ_FLAG_PAGED_ALL, window)
@@ -76,80 +76,87 @@ class PagedCache:
         return self
 
     # ---- the calls ----
-    def _call(self, t: torch.Tensor, heads: int, n_new, n_new_per_seq, row_start) -> Tuple[torch.Tensor, "B.SparqRows"]:
-        """The rows of a call and what says which they are; a workspace that is large enough."""
-        if t.dtype != self.dtype or t.device != self.device:
+    def _rows(self, t: torch.Tensor, heads: int, n_new, n_new_per_seq, row_start) -> "B.SparqRows":
+        """Checks the rows of a call; what says which they are; a workspace that is large enough."""
+        if t.dtype is not self.dtype or t.device != self.device:
             raise ValueError(f"rows must be {self.dtype} on {self.device}, got {t.dtype} on {t.device}")
+        size = t.shape
         if row_start is None:
-            t = t.unsqueeze(2) if t.dim() == 3 else t
-            if t.dim() != 4 or t.shape[0] != self.B or t.shape[1] != heads or t.shape[3] != self.d_h:
-                raise ValueError(f"rows must be [{self.B}, {heads}, n, {self.d_h}], got {tuple(t.shape)}")
-            if n_new is not None and n_new != t.shape[2]:
+            if len(size) != 4 or size[0] != self.B or size[1] != heads or size[3] != self.d_h:
+                raise ValueError(f"rows must be [{self.B}, {heads}, n, {self.d_h}], got {tuple(size)}")
+            n, n_rows = size[2], 0
+            if n_new is not None and n_new != n:
                 raise ValueError("n_new is the rows' third size where they are not packed")
-            n, n_rows = t.shape[2], 0
         else:
-            if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.d_h:
-                raise ValueError(f"packed rows must be [n_rows, {heads}, {self.d_h}], got {tuple(t.shape)}")
+            if len(size) != 3 or size[1] != heads or size[2] != self.d_h:
+                raise ValueError(f"packed rows must be [n_rows, {heads}, {self.d_h}], got {tuple(size)}")
             if n_new is None:
                 raise ValueError("packed rows need n_new, the most rows of a sequence")
-            if row_start.shape != (self.B + 1,):
-                raise ValueError("row_start must be [B + 1]")
-            n, n_rows = n_new, t.shape[0]
-        if n_new_per_seq is not None and n_new_per_seq.shape != (self.B,):
-            raise ValueError("n_new_per_seq must be [B]")
-        for x in (n_new_per_seq, row_start):
-            if x is not None and x.device != self.device:
-                raise ValueError(f"row counts must live on {self.device}")
+            if row_start.shape != (self.B + 1,) or row_start.device != self.device:
+                raise ValueError(f"row_start must be [B + 1] on {self.device}")
+            n, n_rows = n_new, size[0]
+        if n_new_per_seq is not None and (n_new_per_seq.shape != (self.B,) or n_new_per_seq.device != self.device):
+            raise ValueError(f"n_new_per_seq must be [B] on {self.device}")
         if n > self._rows_room:
             need = B.sparq_paged_workspace_bytes(self.shape, n)
             if need > self.workspace.numel():
                 self.workspace = torch.zeros((need,), dtype=torch.uint8, device=self.device)
-                B.sparq_workspace_init(self.workspace, torch.cuda.current_stream(self.device))
+                B.sparq_workspace_init(self.workspace)
             self._rows_room = n
-        return t, B.make_rows(n, n_new_per_seq, row_start, n_rows)
+        return B.make_rows(n, n_new_per_seq, row_start, n_rows)
 
-    def _on(self, stream):
-        return torch.cuda.current_stream(self.device) if stream is None else stream
+    def _elsewhere(self, stream) -> bool:
+        """Whether the current device is another one than the cache's (the calls go to the current one)."""
+        if stream is not None and stream.device != self.device:
+            raise ValueError(f"the stream must be one of {self.device}")
+        return torch.cuda.current_device() != self._index
 
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor, n_new_per_seq: Optional[torch.Tensor] = None,
                row_start: Optional[torch.Tensor] = None, n_new: Optional[int] = None, stream=None) -> None:
         """Write the rows at the last positions of every sequence (heads: H_kv)."""
-        with torch.cuda.device(self.device):
-            k_new, rows = self._call(k_new, self.H_kv, n_new, n_new_per_seq, row_start)
-            v_new, _ = self._call(v_new, self.H_kv, n_new, n_new_per_seq, row_start)
-            B.sparq_paged_append(self.shape, self.cache, rows, k_new, v_new, self.workspace, self._on(stream))
+        if self._elsewhere(stream):
+            with torch.cuda.device(self.device):
+                return self.append(k_new, v_new, n_new_per_seq, row_start, n_new, stream)
+        if row_start is None and k_new.dim() == 3:
+            k_new, v_new = k_new.unsqueeze(2), v_new.unsqueeze(2)
+        rows = self._rows(k_new, self.H_kv, n_new, n_new_per_seq, row_start)
+        B.sparq_paged_append(self.shape, self.cache, rows, k_new, v_new, self.workspace, stream)
 
     def attend(self, q: torch.Tensor, n_new_per_seq: Optional[torch.Tensor] = None, row_start: Optional[torch.Tensor] = None,
                n_new: Optional[int] = None, out: Optional[torch.Tensor] = None, lse: Union[None, bool, torch.Tensor] = None, stream=None):
         """Attention of the last rows of every sequence (heads: H).  lse: True, or a float32 tensor for the logarithms of the
         denominators, [B, H, n] or packed [H, n_rows]; (out, lse) is returned if it is True."""
-        with torch.cuda.device(self.device):
-            q4, rows = self._call(q, self.H, n_new, n_new_per_seq, row_start)
-            if out is None:      # rows that belong to no sequence are not written
-                out = torch.empty_like(q) if n_new_per_seq is None and row_start is None else torch.zeros_like(q)
-            elif out.shape != q.shape:
-                raise ValueError("out must have q's shape")
-            o4, _ = self._call(out, self.H, n_new, n_new_per_seq, row_start)
+        if self._elsewhere(stream):
+            with torch.cuda.device(self.device):
+                return self.attend(q, n_new_per_seq, row_start, n_new, out, lse, stream)
+        if out is None:          # rows that belong to no sequence are not written
+            out = torch.empty_like(q) if n_new_per_seq is None and row_start is None else torch.zeros_like(q)
+        elif out.shape != q.shape or out.dtype is not q.dtype or out.device != q.device:
+            raise ValueError("out must have q's shape, type and device")
+        q4, o4 = (q.unsqueeze(2), out.unsqueeze(2)) if row_start is None and q.dim() == 3 else (q, out)
+        rows = self._rows(q4, self.H, n_new, n_new_per_seq, row_start)
+        lse_out = None
+        if lse is not None and lse is not False:
             size = (self.H, q.shape[0]) if row_start is not None else (self.B, self.H, q4.shape[2])
-            lse_out = None
-            if lse is not None and lse is not False:
-                lse_out = torch.full(size, -float("inf"), dtype=torch.float32, device=self.device) if lse is True else lse
-                if lse_out.shape != size or lse_out.device != self.device:
-                    raise ValueError(f"lse must be {size} on {self.device}")
-            B.sparq_paged_attention(self.shape, self.cache, rows, q4, o4, lse_out, self.workspace, self._on(stream))
-            return (out, lse_out) if lse is True else out
+            lse_out = torch.full(size, -float("inf"), dtype=torch.float32, device=self.device) if lse is True else lse
+            if lse_out.shape != size or lse_out.device != self.device:
+                raise ValueError(f"lse must be {size} on {self.device}")
+        B.sparq_paged_attention(self.shape, self.cache, rows, q4, o4, lse_out, self.workspace, stream)
+        return (out, lse_out) if lse is True else out
 
     def read(self, K_out: torch.Tensor, V_out: torch.Tensor, first: Optional[torch.Tensor] = None, n_per_seq: Optional[torch.Tensor] = None,
              row_start: Optional[torch.Tensor] = None, n_new: Optional[int] = None, stream=None):
         """Rows first[b] .. (0 .. without it) of every sequence as 16-bit rows, into K_out and V_out (heads: H_kv); they are returned."""
-        with torch.cuda.device(self.device):
-            k, rows = self._call(K_out, self.H_kv, n_new, n_per_seq, row_start)
-            v, _ = self._call(V_out, self.H_kv, n_new, n_per_seq, row_start)
-            if first is not None and first.shape != (self.B,):
-                raise ValueError("first must be [B]")
-            B.sparq_paged_read(self.shape, self.cache, rows, first, k, v, self.workspace, self._on(stream))
-            return K_out, V_out
+        if self._elsewhere(stream):
+            with torch.cuda.device(self.device):
+                return self.read(K_out, V_out, first, n_per_seq, row_start, n_new, stream)
+        k, v = (K_out.unsqueeze(2), V_out.unsqueeze(2)) if row_start is None and K_out.dim() == 3 else (K_out, V_out)
+        rows = self._rows(k, self.H_kv, n_new, n_per_seq, row_start)
+        if first is not None and (first.shape != (self.B,) or first.device != self.device):
+            raise ValueError(f"first must be [B] on {self.device}")
+        B.sparq_paged_read(self.shape, self.cache, rows, first, k, v, self.workspace, stream)
+        return K_out, V_out
 
     def error_flags(self) -> int:
         with torch.cuda.device(self.device):
-            return B.sparq_async_error(self.workspace, torch.cuda.current_stream(self.device))
+            return B.sparq_async_error(self.workspace)

@@ -73,7 +73,7 @@ def test_pointers_rows_strides_and_workspaces():
     assert calls(r=rows(0)) == {E} and calls(r=rows(-1)) == {E} and calls(r=rows(2, 5, FAKE, FAKE)) == {E} and calls(r=rows(2, 0, None, FAKE)) == {E}
     assert calls(r=rows(1 << 29)) == {B.SPARQ_EUNSUPPORTED}
     for s in (strides(seq=-8), strides(head=-128), strides(row=-8), strides(seq=1020), strides(head=130), strides(row=4)):
-        assert calls(s=s) == {E}
+        assert calls(r=rows(2), s=s) == {E}
     # what is written must not lie on top of itself; what is read may
     for s in (strides(seq=0), strides(head=0), strides(head=64)):
         assert calls(so=s, skip=("append",)) == {E}
