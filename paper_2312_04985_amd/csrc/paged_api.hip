@@ -76,10 +76,13 @@ AttendPlan attend_plan(const sparq_paged_shape* s, int n, bool counted) {
 
 int tokens_tile(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
 
-// Workgroups of the first kernel: what runs at once, and no more than 64 for a unit, whose last one puts their results together.
+// Workgroups of the first kernel: what runs at once, but no more than 32 for a unit, whose last one puts their results together, or 64 while
+// that keeps to one per CU (us, 32 / 64 for each, 32 768 positions of 128 channels: 8 units of e4m3 pages 25.2 / 28.3, of 16 bits 32.3 / 36.0;
+// 30 000 of 64, 4 units of int8 pages 23.7 / 19.4).
 int tokens_workgroups(const sparq_paged_shape* s, int tile) {
   const int64_t units = (int64_t)s->B * s->H_kv, most = 256 * tokens_per_cu(s->d_h, tile);
-  return (int)(units * 64 < most ? units * 64 : most);
+  const int64_t one_per_cu = units * 64 < 256 ? units * 64 : 256, want = units * 32 > one_per_cu ? units * 32 : one_per_cu;
+  return (int)(want < most ? want : most);
 }
 
 // Row tiles of the second kernel per (sequence, KV head) if a workgroup serves each, 0 if they are cut into equal parts of the work:
