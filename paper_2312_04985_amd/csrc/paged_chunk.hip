@@ -208,8 +208,10 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     const uint16_t* qp = reinterpret_cast<const uint16_t*>(a.q) + row_offset(a.qs, packed, b, r.row0, head, t) + half * 8;
 #pragma unroll
     for (int s = 0; s < DH / 16; ++s) qf[s] = *reinterpret_cast<const uint4*>(qp + s * 16);
-    float c_row = kLog2e / sqrtf((float)DH);                   // scores to exponents of 2
-    if constexpr (PT != kPages16 && std::is_same_v<T, BF16>) query_to_half<32>(qf, c_row);
+    const float c = kLog2e / sqrtf((float)DH);                 // scores to exponents of 2
+    float lift = 1.0f;
+    if constexpr (PT != kPages16 && std::is_same_v<T, BF16>) lift = query_to_half<32>(qf);
+    const bool lifted = __ballot(lift != 1.0f) != 0;           // some row of the wave
 
     f32x16 O[ND];
 #pragma unroll
@@ -273,9 +275,10 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
         }
         if (part == 0 && lane < 16) {
           const float v = value_scale(csv);
-          lds.s_k[buf][group * 16 + lane] = csk;
+          lds.s_k[buf][group * 16 + lane] = csk * c;
           lds.s_log[buf][group * 16 + lane] = log2_normal(v);
-          lds.s_inv[buf][group * 16 + lane] = 1.0f / v;
+          // (a scale that is no number makes NaN of what sees it by its logarithm; its inverse must leave the 0 of what does not)
+          lds.s_inv[buf][group * 16 + lane] = v < INFINITY ? 1.0f / v : 0.0f;
         }
       }
     };
@@ -325,12 +328,18 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
         }
         __builtin_amdgcn_s_setprio(0);
         if constexpr (PT != kPages16) {
+          if (std::is_same_v<T, BF16> && lifted) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) S[i][e] *= lift;
+          }
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const int j = 32 * i + 8 * (e / 4) + e % 4 + 4 * half;
-              S[i][e] = fmaf(S[i][e], lds.s_k[buf][j] * c_row, lds.s_log[buf][j]);
+              S[i][e] = fmaf(S[i][e], lds.s_k[buf][j], lds.s_log[buf][j]);
             }
         }
         const bool masked = p0 < w_last.lo || p0 + kTile > w_first.hi;
@@ -342,13 +351,13 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
             for (int e = 0; e < 16; ++e)
               if (at0 + (32 * i + 8 * (e / 4) + e % 4) >= len) S[i][e] = -INFINITY;
         }
-        const float c = PT == kPages16 ? c_row : 1.0f;         // (8-bit pages: in the exponents already)
+        const float c_max = PT == kPages16 ? c : 1.0f;         // (8-bit pages: in the exponents already)
         float mx = fmaxf(S[0][0], S[1][0]);
 #pragma unroll
         for (int e = 1; e < 16; ++e) mx = fmaxf(fmaxf(mx, S[0][e]), S[1][e]);
         float m_a, m_b;
         lane_pair<32>(mx, m_a, m_b);
-        const float m_new = fmaxf(m_a, m_b) * c;
+        const float m_new = fmaxf(m_a, m_b) * c_max;
         // the maximum is followed only when it rises by more than 8: weights are at most 2^8 then, and most tiles rescale nothing
         if (__ballot(m_new > m_ref + 8.0f)) {
           const float m_to = fmaxf(m_new, m_ref);
@@ -374,12 +383,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int j = 32 * i + 8 * (e / 4) + e % 4;
-              float inv = lds.s_inv[buf][j + 4 * half];
-              if (masked && at0 + j >= len) inv = 0.0f;        // (whatever the scale of a position that is not seen: 0 times it)
-              l = fmaf(S[i][e], inv, l);
-            }
+            for (int e = 0; e < 16; ++e) l = fmaf(S[i][e], lds.s_inv[buf][32 * i + 8 * (e / 4) + e % 4 + 4 * half], l);
         }
       }
 
@@ -419,27 +423,29 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 
       // ---- output ----
       if (active) {
-        uint4 vf[2][ND];                                       // the values of 16 positions and of the next 16
+        // the values of 16 positions and of the next 16 (8-bit pages: the next tile's codes are in the registers for those)
+        constexpr int AHEAD = PT == kPages16 ? 1 : 0;
+        uint4 vf[1 + AHEAD][ND];
         auto fetch = [&](int sl) {
           const int row = sl * 16 + 4 * half + (lane & 15) / 4;
 #pragma unroll
           for (int j = 0; j < ND; ++j) {
             const int piece = 4 * j + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), sub = (lane & 1) * 4;
             const uint2 v0 = lds_read_transposed(&vt[value_piece<DH>(row, piece) + sub]), v1 = lds_read_transposed(&vt[value_piece<DH>(row + 8, piece) + sub]);
-            vf[sl % 2][j] = make_uint4(v0.x, v0.y, v1.x, v1.y);
+            vf[sl % (1 + AHEAD)][j] = make_uint4(v0.x, v0.y, v1.x, v1.y);
           }
         };
-        fetch(0);
+        if (AHEAD) fetch(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int sl = 0; sl < 4; ++sl) {
-          if (sl < 3) fetch(sl + 1);
+          if (sl + AHEAD < 4) fetch(sl + AHEAD);
           const int e0 = sl % 2 * 8;
           const f32x16& w = S[sl / 2];
           const uint4 pw = make_uint4(narrow2<E>(w[e0], w[e0 + 1]), narrow2<E>(w[e0 + 2], w[e0 + 3]), narrow2<E>(w[e0 + 4], w[e0 + 5]), narrow2<E>(w[e0 + 6], w[e0 + 7]));
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int j = 0; j < ND; ++j) O[j] = mfma_32x32x16<E>(vf[sl % 2][j], pw, O[j]);
+          for (int j = 0; j < ND; ++j) O[j] = mfma_32x32x16<E>(vf[sl % (1 + AHEAD)][j], pw, O[j]);
           __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);

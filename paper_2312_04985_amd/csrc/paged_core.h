@@ -36,10 +36,11 @@ template <class T> __device__ __forceinline__ bool has_special(const uint4& v) {
 // A value's scale as the attention uses it: a scale of 0 (rows of zeros that another program wrote) has no logarithm; NaN stays.
 __device__ __forceinline__ float value_scale(float s) { return s < kLeastMagnitude / 1024.0f ? kLeastMagnitude / 1024.0f : s; }
 
-// bf16 queries for products of fp16 (8-bit pages): a row, whose pieces lie in the lanes l ^ X, l ^ 2 X .. l ^ 32, is brought to a largest
-// finite magnitude in [2^14, 2^15) by a power of 2.  There fp16 holds every bf16 value down to 2^-32 of it exactly, and the
-// rest to within 2^-40 of it.  c, which turns the row's scores into exponents of 2, gets the inverse.
-template <int X, int N> __device__ __forceinline__ void query_to_half(uint4 (&q)[N], float& c) {
+// bf16 queries for products of fp16 (8-bit pages): a row, whose pieces lie in the lanes l ^ X, l ^ 2 X .. l ^ 32, is multiplied by a power
+// of 2, the inverse of which is returned: 1 where its largest finite magnitude lies in [2^-4, 2^15), as those of most rows do, otherwise
+// what brings it into [2^14, 2^15).  fp16 then holds every bf16 value of 2^-17 and more exactly, the others to within 2^-25: 2^-21 of the row's
+// largest, less than the sums' own roundings.
+template <int X, int N> __device__ __forceinline__ float query_to_half(uint4 (&q)[N]) {
   uint32_t top = 0;
 #pragma unroll
   for (int s = 0; s < N; ++s)
@@ -53,14 +54,15 @@ template <int X, int N> __device__ __forceinline__ void query_to_half(uint4 (&q)
   for (int o = X; o < kWave; o <<= 1) { const uint32_t other = __shfl_xor(top, o); top = other > top ? other : top; }
   int e = (int)(top >> 7) - 127;                               // exponent of the largest finite magnitude
   e = e < -112 ? -112 : e;                                     // (2^(14 - e) stays a float)
-  const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
-  c *= __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+  const int lift = e >= -4 && e < 15 ? 0 : 14 - e;
+  const float up = __uint_as_float((uint32_t)(lift + 127) << 23);
 #pragma unroll
   for (int s = 0; s < N; ++s) {
     float f[8];
     unpack8<BF16>(q[s], f);
     q[s] = make_uint4(narrow2<F16>(f[0] * up, f[1] * up), narrow2<F16>(f[2] * up, f[3] * up), narrow2<F16>(f[4] * up, f[5] * up), narrow2<F16>(f[6] * up, f[7] * up));
   }
+  return __uint_as_float((uint32_t)(127 - lift) << 23);
 }
 
 // The positions [lo, hi) that row t of a sequence sees.  Both rise with t.

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(TT, tokens_per_cu(DH, 16 * NT)) void paged_tokens(c
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) qf[nt][kk] = *reinterpret_cast<const uint4*>(qp + (PT == kPages16 ? kk * 32 : kk / 2 * 64 + kk % 2 * 8));
       c_row[nt] = kLog2e / sqrtf((float)DH);
-      if constexpr (PT != kPages16 && std::is_same_v<T, BF16>) query_to_half<16>(qf[nt], c_row[nt]);
+      if constexpr (PT != kPages16 && std::is_same_v<T, BF16>) c_row[nt] *= query_to_half<16>(qf[nt]);
       m_ref[nt] = -INFINITY; l[nt] = 0.0f;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) O[nt][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
