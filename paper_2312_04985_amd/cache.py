@@ -39,6 +39,7 @@ class DecodeCache:
         self.cache = B.make_cache(self.K, self.Kt, self.V, self.v_mean, self.seq_lens)
         self._v_mean_alt = None      # second (v_mean, seq_lens) pair for the one-launch step, made on first use
         self._seq_lens_alt = None
+        self._paged = None           # K and V as pages, made on the first prefill
 
     def with_params(self, r: int, k: int, flags: int = 0, local_window: int = 0, S_bound: int = 0):
         """The same buffers seen through another (r, k, flags, local window, bound on the lengths) setting."""
@@ -59,6 +60,19 @@ class DecodeCache:
         """k_new, v_new: [B, H_kv, n_new, d_h] (or [B, H_kv, d_h] for one row)."""
         n_new = 1 if k_new.dim() == 3 else k_new.shape[2]
         B.sparq_kv_append(self.shape, self.cache, k_new, v_new, n_new, n_new_per_seq, self.workspace, stream)
+
+    def prefill(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, n_new_per_seq: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, stream=None):
+        """Append rows k_new, v_new [B, H_kv, n, d_h] and attend with their queries q [B, H, n, d_h] (any order with contiguous channels) over all
+        cached rows, causally: a prompt, or the next chunk of one.  The attention is sparq_paged_attention's; K and V are pages of S_max positions to it."""
+        if self.tiled:
+            raise ValueError("the tiled key layout has no rows for the attention of a chunk")
+        if self._paged is None:
+            from .paged import PagedCache
+            pages = torch.arange(self.B, dtype=torch.int32, device=self.device)[:, None]
+            self._paged = PagedCache.over(self.K, self.V, pages, self.seq_lens, self.H, self.dtype)
+        self.append(k_new, v_new, n_new_per_seq, stream)
+        return self._paged.with_lengths(self.seq_lens).attend(q, n_new_per_seq, out=out, stream=stream)
 
     def decode(self, q: torch.Tensor, k_per_seq: Optional[torch.Tensor] = None, aux: bool = False,
                idx_stride: Optional[int] = None, out: Optional[torch.Tensor] = None, stream=None):
@@ -113,4 +127,4 @@ class DecodeCache:
         return rows
 
     def error_flags(self) -> int:
-        return B.sparq_async_error(self.workspace)
+        return B.sparq_async_error(self.workspace) | (0 if self._paged is None else self._paged.error_flags())

@@ -98,7 +98,7 @@ struct ChunkPlan {
   int workgroups;
   int tiles;                                            // row tiles per (sequence, KV head), each by a workgroup of its own; 0: equal parts of the work
   float* partials;                                      // ... which leave [workgroups][2][2 chunk_rows lanes][d_h / 2 + 4] for each other
-  int32_t* tickets;                                     // [workgroups], 0 between launches
+  int32_t* tickets;                                     // [2][workgroups], 0 between launches
 };
 
 hipError_t launch_paged_append(const PagedRowsArgs& a, int dtype, int page_type, hipStream_t s);

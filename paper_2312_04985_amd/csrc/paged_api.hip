@@ -129,7 +129,7 @@ int check_call(const sparq_paged_shape* s, const sparq_paged_cache* c, const spa
   return SPARQ_OK;
 }
 
-static_assert(kTokensWorkgroups <= kTickets, "a counter per workgroup");
+static_assert(kTokensWorkgroups <= kTickets && 2 * 256 * chunk_per_cu(64) <= kTickets, "the workgroups' counters");
 
 PagedArgs paged_args(const sparq_paged_shape* s, const sparq_paged_cache* c, const sparq_rows* r, void* ws) {
   PagedArgs p{};

@@ -28,6 +28,7 @@ namespace {
 constexpr int kTile = 64;               // positions per tile
 // What a row tile costs besides its tiles of positions (queries, first loads, results), in tiles.
 constexpr int kStart = 4;
+constexpr int kGather = 8;              // results that a workgroup puts together at a time
 constexpr int kWaves = chunk_rows / 32; // waves of a workgroup
 
 // c[m][n] += sum_k a[m][k] b[n][k] over 16 k: lane l holds a[l % 32], b[l % 32] at k = 8 (l / 32) .. + 7 and
@@ -460,21 +461,22 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
       const int first_wg = k0 == 0 ? me : (int)((tile_at + kStart) / share), last_wg = tile_end <= end ? me : (int)((tile_end - 1) / share);
       constexpr int SLOT = NTH * (DH / 2 + 4);                 // floats: a lane's DH / 2 numerators, its maximum and its part of the denominator
       auto slot_of = [&](int wg) { return partials + ((size_t)wg * 2 + (wg == first_wg ? 1 : 0)) * SLOT; };
-      float* dst = slot_of(me);
+      auto store = [&](float* dst) {
 #pragma unroll
-      for (int j = 0; j < ND; ++j)
+        for (int j = 0; j < ND; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) store_agent4(dst, (uint32_t)((j * 4 + q) * NTH + tid) * 16, make_float4(O[j][4 * q], O[j][4 * q + 1], O[j][4 * q + 2], O[j][4 * q + 3]));
-      store_agent4(dst, (uint32_t)(ND * 4 * NTH + tid) * 16, make_float4(m_ref, l, 0.0f, 0.0f));
-      write = last_to_arrive(plan.tickets + first_wg, last_wg - first_wg + 1, &lds.flag);
-      if (write) {                                             // in the order of the line, whoever is last
+          for (int q = 0; q < 4; ++q) store_agent4(dst, (uint32_t)((j * 4 + q) * NTH + tid) * 16, make_float4(O[j][4 * q], O[j][4 * q + 1], O[j][4 * q + 2], O[j][4 * q + 3]));
+        store_agent4(dst, (uint32_t)(ND * 4 * NTH + tid) * 16, make_float4(m_ref, l, 0.0f, 0.0f));
+      };
+      // the results of every `step`-th workgroup from wg on, in the order of the line, whoever is last
+      auto gather = [&](int wg, int step, int to_wg) {
         m_ref = -INFINITY; l = 0.0f;
 #pragma unroll
         for (int j = 0; j < ND; ++j)
 #pragma unroll
           for (int i = 0; i < 16; ++i) O[j][i] = 0.0f;
 #pragma unroll 1
-        for (int wg = first_wg; wg <= last_wg; ++wg) {
+        for (; wg <= to_wg; wg += step) {
           const float* src = slot_of(wg);
           const float4 st = load_agent4(src, (uint32_t)(ND * 4 * NTH + tid) * 16);
           const float m_to = fmaxf(m_ref, st.x), f = weight_exp2(m_ref, m_to), g = weight_exp2(st.x, m_to);
@@ -493,6 +495,18 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
             }
           }
         }
+      };
+      // The last of eight neighbours puts theirs together, the last of those that did so puts these together: one workgroup takes 2 us for a result
+      // (128 rows over 32 768 positions, 64 workgroups to each row tile: 133 us by one of them).
+      // (A counter per group at its first workgroup: a group of one, which another row tile's may share its workgroup with, needs none.)
+      const int group0 = first_wg + (me - first_wg) / kGather * kGather, group1 = group0 + kGather - 1 < last_wg ? group0 + kGather - 1 : last_wg;
+      store(slot_of(me));
+      write = group0 == group1 || last_to_arrive(plan.tickets + group0, group1 - group0 + 1, &lds.flag);
+      if (write && group0 != group1) gather(group0, 1, group1);
+      if (write && last_wg - first_wg >= kGather) {
+        if (group0 != group1) store(slot_of(group0));
+        write = last_to_arrive(plan.tickets + G + first_wg, (last_wg - first_wg) / kGather + 1, &lds.flag);
+        if (write) gather(first_wg, kGather, last_wg);
       }
     }
 

@@ -9,6 +9,7 @@ from typing import Optional, Union
 import torch
 
 from . import binding as B
+from .cache import DecodeCache
 
 PAGE_TYPES = {"16": B.SPARQ_PAGES_16, "i8": B.SPARQ_PAGES_I8, "e4m3": B.SPARQ_PAGES_E4M3}
 CODE_TYPES = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
@@ -65,7 +66,7 @@ class PagedCache:
         self.shape = B.make_paged_shape(Bsz, H, H_kv, d_h, page_size, n_pages, max_pages, dtype, PAGE_TYPES[self.pages],
                                         0 if causal else B.SPARQ_FLAG_PAGED_ALL, window)
         self.workspace = torch.zeros((B.sparq_paged_workspace_bytes(self.shape, 1),), dtype=torch.uint8, device=self.device)
-        self._rows_room = 1
+        self._rows_room, self._outgrown = 1, []
         with torch.cuda.device(self.device):
             B.sparq_workspace_init(self.workspace)
 
@@ -75,8 +76,17 @@ class PagedCache:
         self._rows_room = 0
         return self
 
+    def with_lengths(self, seq_lens: torch.Tensor) -> "PagedCache":
+        """The same pages with another tensor of lengths."""
+        if seq_lens.shape != (self.B,) or seq_lens.device != self.device:
+            raise ValueError(f"seq_lens must be [B] on {self.device}")
+        if seq_lens is not self.seq_lens:
+            self.seq_lens = seq_lens
+            self.cache = B.make_paged_cache(self.K, self.V, self.K_scale, self.V_scale, self.page_table, seq_lens)
+        return self
+
     # ---- the calls ----
-    def _rows(self, t: torch.Tensor, heads: int, n_new, n_new_per_seq, row_start) -> "B.SparqRows":
+    def _rows(self, t: torch.Tensor, heads: int, n_new, n_new_per_seq, row_start, stream) -> "B.SparqRows":
         """Checks the rows of a call; what says which they are; a workspace that is large enough."""
         if t.dtype is not self.dtype or t.device != self.device:
             raise ValueError(f"rows must be {self.dtype} on {self.device}, got {t.dtype} on {t.device}")
@@ -98,12 +108,19 @@ class PagedCache:
         if n_new_per_seq is not None and (n_new_per_seq.shape != (self.B,) or n_new_per_seq.device != self.device):
             raise ValueError(f"n_new_per_seq must be [B] on {self.device}")
         if n > self._rows_room:
-            need = B.sparq_paged_workspace_bytes(self.shape, n)
-            if need > self.workspace.numel():
-                self.workspace = torch.zeros((need,), dtype=torch.uint8, device=self.device)
-                B.sparq_workspace_init(self.workspace)
-            self._rows_room = n
+            self._grow(n, stream)
         return B.make_rows(n, n_new_per_seq, row_start, n_rows)
+
+    def _grow(self, n: int, stream) -> None:
+        """Room for calls of n rows per sequence.  The old workspace stays: calls in flight and captured ones go on using it."""
+        need = B.sparq_paged_workspace_bytes(self.shape, n)
+        if need > self.workspace.numel():
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the workspace is too small for this call and cannot be replaced during a capture: make a call of this size before it")
+            self._outgrown.append(self.workspace)
+            self.workspace = torch.empty((need,), dtype=torch.uint8, device=self.device)
+            B.sparq_workspace_init(self.workspace, stream)
+        self._rows_room = n
 
     def _elsewhere(self, stream) -> bool:
         """Whether the current device is another one than the cache's (the calls go to the current one)."""
@@ -119,7 +136,7 @@ class PagedCache:
                 return self.append(k_new, v_new, n_new_per_seq, row_start, n_new, stream)
         if row_start is None and k_new.dim() == 3:
             k_new, v_new = k_new.unsqueeze(2), v_new.unsqueeze(2)
-        rows = self._rows(k_new, self.H_kv, n_new, n_new_per_seq, row_start)
+        rows = self._rows(k_new, self.H_kv, n_new, n_new_per_seq, row_start, stream)
         B.sparq_paged_append(self.shape, self.cache, rows, k_new, v_new, self.workspace, stream)
 
     def attend(self, q: torch.Tensor, n_new_per_seq: Optional[torch.Tensor] = None, row_start: Optional[torch.Tensor] = None,
@@ -134,7 +151,7 @@ class PagedCache:
         elif out.shape != q.shape or out.dtype is not q.dtype or out.device != q.device:
             raise ValueError("out must have q's shape, type and device")
         q4, o4 = (q.unsqueeze(2), out.unsqueeze(2)) if row_start is None and q.dim() == 3 else (q, out)
-        rows = self._rows(q4, self.H, n_new, n_new_per_seq, row_start)
+        rows = self._rows(q4, self.H, n_new, n_new_per_seq, row_start, stream)
         lse_out = None
         if lse is not None and lse is not False:
             size = (self.H, q.shape[0]) if row_start is not None else (self.B, self.H, q4.shape[2])
@@ -151,12 +168,24 @@ class PagedCache:
             with torch.cuda.device(self.device):
                 return self.read(K_out, V_out, first, n_per_seq, row_start, n_new, stream)
         k, v = (K_out.unsqueeze(2), V_out.unsqueeze(2)) if row_start is None and K_out.dim() == 3 else (K_out, V_out)
-        rows = self._rows(k, self.H_kv, n_new, n_per_seq, row_start)
+        rows = self._rows(k, self.H_kv, n_new, n_per_seq, row_start, stream)
         if first is not None and (first.shape != (self.B,) or first.device != self.device):
             raise ValueError(f"first must be [B] on {self.device}")
         B.sparq_paged_read(self.shape, self.cache, rows, first, k, v, self.workspace, stream)
         return K_out, V_out
 
+    def to_decode_cache(self, n: int, S_max: int, r: int, k: int, flags: int = 0) -> DecodeCache:
+        """A SparQ cache with the rows of these pages (n: the most positions of a sequence): read back, then appended."""
+        c = DecodeCache(self.B, self.H, self.H_kv, S_max, self.d_h, r, k, self.dtype, device=self.device, flags=flags)
+        K, V = (torch.empty((self.B, self.H_kv, n, self.d_h), dtype=self.dtype, device=self.device) for _ in range(2))
+        self.read(K, V, n_per_seq=self.seq_lens)
+        c.append(K, V, self.seq_lens)
+        return c
+
     def error_flags(self) -> int:
+        """The SPARQ_ERR_* bits of the calls so far (waits for the current stream), which are cleared."""
         with torch.cuda.device(self.device):
-            return B.sparq_async_error(self.workspace)
+            flags = 0
+            for w in self._outgrown + [self.workspace]:
+                flags |= B.sparq_async_error(w)
+            return flags
