@@ -4,7 +4,9 @@
 // largest magnitude (fp32 division), and code = the nearest code to x (qmax / a): one multiplication by a quotient that is
 // rounded once, so that the codes are those of the same three operations anywhere.
 // Bound by HBM: every byte is moved once, nothing is kept.  d_h / 8 lanes share a row (16 bytes each of the 16-bit side), and
-// a thread has its part of the K row and of the V row in flight together.
+// a thread has its part of the K row and of the V row in flight together.  Rows that are read back are stored past the caches, which
+// leaves these to the pages: 31 777 rows of 8 KV heads from e4m3 pages (197 MB) 32.5 us (6.1 TB/s; 45.4 with ordinary stores, 41.7 with
+// loads past the caches too).
 #include "paged_codes.h"
 
 namespace sparq {
@@ -110,8 +112,8 @@ __global__ __launch_bounds__(RT) void paged_read(const PagedRowsArgs a) {
   if (row < 0) return;
   const uint4 k = load_row<T, PT, DH>(a.p.K, a.p.K_scale, row, it.c0), v = load_row<T, PT, DH>(a.p.V, a.p.V_scale, row, it.c0);
   const int64_t to = row_offset(a.s, a.p.row_start != nullptr, it.b, it.r.row0, it.head, it.t) + it.c0;
-  *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.k) + to) = k;
-  *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.v) + to) = v;
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, k), reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.k) + to));
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.v) + to));
 }
 
 template <class T, int PT, int DH>
