@@ -20,49 +20,12 @@
 // us, row tiles / the line (128 channels, f16; row tiles of all KV heads): 32 heads of 512 rows behind 8192 positions, 256 row tiles 216 / 194,
 // 384 278 / 311, 512 318 / 321, 640 474 / 515, 768 514 / 592, 1024 642 / 732, 1536 914 / 1117; prompts of 1024, 2048, 4096 and 8192, 256 35.5 / 40,
 // 512 75.6 / 71, 1024 212 / 215, 2048 622 / 680; 8 KV heads of 4 heads, prompts of 4096, 1024 162 / 180.
-#include "paged_core.h"
+#include "paged_tiles.h"
 
 namespace sparq {
 namespace {
 
-constexpr int kTile = 64;               // positions per tile
-// What a row tile costs besides its tiles of positions (queries, first loads, results), in tiles.
-constexpr int kStart = 4;
-constexpr int kGather = 8;              // results that a workgroup puts together at a time
 constexpr int kWaves = chunk_rows / 32; // waves of a workgroup
-
-// c[m][n] += sum_k a[m][k] b[n][k] over 16 k: lane l holds a[l % 32], b[l % 32] at k = 8 (l / 32) .. + 7 and
-// c[8 (i / 4) + 4 (l / 32) + i % 4][l % 32]
-template <class T> __device__ __forceinline__ f32x16 mfma_32x32x16(const uint4& a, const uint4& b, f32x16 c);
-template <> __device__ __forceinline__ f32x16 mfma_32x32x16<F16>(const uint4& a, const uint4& b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-template <> __device__ __forceinline__ f32x16 mfma_32x32x16<BF16>(const uint4& a, const uint4& b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Rows of DH elements in LDS in pieces of 8 (16 bytes).  Keys are read by 32 rows at one piece, values by 8 rows at 4
-// neighbouring pieces: both are spread over the banks by changing the pieces' places with the row.
-template <int DH> __device__ __forceinline__ int key_turn(int row) { return row & (DH / 8 - 1) & 15; }
-template <int DH> __device__ __forceinline__ int value_turn(int row) { return DH == 64 ? ((row & 1) << 2) | ((row >> 1) & 3) : ((row & 3) << 2) | ((row >> 2) & 3); }
-template <int DH> __device__ __forceinline__ int key_piece(int row, int piece) { return row * DH + ((piece ^ key_turn<DH>(row)) << 3); }
-template <int DH> __device__ __forceinline__ int value_piece(int row, int piece) { return row * DH + ((piece ^ value_turn<DH>(row)) << 3); }
-
-// 16 bytes per lane from memory (base + the lane's offset) into LDS at `to` + 16 lane, without a way through registers: the
-// instruction has no result but what tile_barrier waits for.  (The builtin for it makes every transposing read wait for all
-// such loads, those into the other buffer too: the prompt of 8192 took 820 us with it.)
-__device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, void* to) {
-  typedef __attribute__((address_space(3))) void lvoid;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"((uint32_t)(uintptr_t)(lvoid*)to), "v"(off), "s"(base) : "memory");
-}
-
-// All of this wave's loads have arrived and its LDS accesses are done; then all waves' have.
-__device__ __forceinline__ void tile_barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070);                          // vmcnt(0) lgkmcnt(0)
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
 
 template <class T, int PT, int DH>
 __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(const PagedAttendArgs a, const ChunkPlan plan, const Divider by_G) {
@@ -76,8 +39,8 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
   struct Lds {
     uint16_t Kt[2][kTile * DH], Vt[2][kTile * DH];
     float s_k[2][kTile], s_log[2][kTile], s_inv[2][kTile];     // 8-bit pages: scale of the key, log2 and inverse of the value's
-    int64_t sum_w[NW];
-    int begin[4], found[NW], flag;
+    LineLds<NW> line;
+    int found[NW], flag;
   };
   __shared__ __align__(16) Lds lds;
   const PagedArgs& p = a.p;
@@ -86,106 +49,26 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
   const int G = plan.workgroups;
   float* const partials = plan.partials;
 
-  const int lane0 = thread & 63;
-  auto rows_of = [&](int b) { return seq_rows(p.seq_lens[b], p.bound, p.n, p.n_per_seq, p.row_start, p.n_rows, b); };
-  auto tiles_of = [&](const SeqRows& r) { const int M = r.n * a.group; return M <= a.skip_rows ? 0 : (M + ROWS - 1) / ROWS; };
-  // The line is counted in tiles of 64 positions: those that row tile k sees, from position `from` on (one at least: rows that see
-  // nothing are written too), behind kStart that stand for its start and end.
-  auto steps_of = [&](const SeqRows& r, int k, int& from, int& to) {
-    const int M = r.n * a.group, m0 = k * ROWS, m1 = m0 + ROWS < M ? m0 + ROWS : M;
-    from = seen_by(a, r, divided(m0, a.by_group)).lo & ~(kTile - 1);
-    to = seen_by(a, r, divided(m1 - 1, a.by_group)).hi;
-    return kStart + (to - from <= kTile ? 1 : (to - from + kTile - 1) / kTile);
-  };
-  auto steps_of_unit = [&](const SeqRows& r) -> int64_t {      // by all lanes of a wave together
-    const int n_tiles = tiles_of(r);
-    int64_t sum = 0;
-    int from, to;
-    for (int k = lane0; k < n_tiles; k += kWave) sum += steps_of(r, k, from, to);
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o);
-    return sum;
-  };
-  // ---- this workgroup's part: [begin, end) of the line, or one row tile whole ----
-  int me = blockIdx.x;
-  int64_t share = 1, begin = 0, end = 0;
-  if (plan.tiles) {
-    // Workgroups are dealt round-robin to the 8 XCDs: eight (sequence, KV head) units at a time, the last row tiles, which see most, first.
-    const int units = p.B * p.H_kv, eight = blockIdx.x / (8 * plan.tiles), in_eight = blockIdx.x - eight * 8 * plan.tiles;
-    const int width = units - eight * 8 < 8 ? units - eight * 8 : 8, up = in_eight / width, unit = eight * 8 + in_eight - up * width;
-    const int b0 = divided(unit, p.by_H_kv), k = plan.tiles - 1 - up;
-    const SeqRows r = rows_of(b0);
-    if (r.err && k == 0 && unit == b0 * p.H_kv && thread == 0) atomicOr(p.err, r.err);
-    if (k >= tiles_of(r)) return;
-    int from, to;
-    end = steps_of(r, k, from, to);
-    if (thread == 0) { lds.begin[0] = b0; lds.begin[1] = unit - b0 * p.H_kv; lds.begin[2] = k; lds.begin[3] = 0; }
-    __syncthreads();
-  } else {
-    // Consecutive parts of the line share rows of the cache; so that they share an L2 too, each XCD takes an eighth of the line.
-    if (G % 8 == 0) me = (int)(blockIdx.x % 8) * (G / 8) + (int)blockIdx.x / 8;
-    const int per = (p.B + NW - 1) / NW, b_first = wave * per, b_last = b_first + per < p.B ? b_first + per : p.B;
-    int64_t mine = 0;
-    for (int b = b_first; b < b_last; ++b) {
-      const SeqRows r = rows_of(b);
-      if (r.err && me == 0 && lane0 == 0) atomicOr(p.err, r.err);
-      mine += steps_of_unit(r);
-    }
-    if (lane0 == 0) lds.sum_w[wave] = mine;
-    __syncthreads();
-    int64_t before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) { before += w < wave ? lds.sum_w[w] : 0; total += lds.sum_w[w]; }
-    before *= p.H_kv; total *= p.H_kv;
-    share = total < INT32_MAX - G ? (int64_t)divided((int)total + G - 1, by_G) : (total + G - 1) / G;
-    begin = (int64_t)me * share;
-    end = begin + share < total ? begin + share : total;
-    if (begin >= end) return;
-    if (before <= begin && begin < before + mine * p.H_kv) {     // one wave
-      int64_t at = before, c = 1;
-      int b = b_first;
-      for (; b < b_last; ++b) {
-        c = steps_of_unit(rows_of(b));
-        if (begin < at + c * p.H_kv || b == b_last - 1) break;
-        at += c * p.H_kv;
-      }
-      const int64_t off = begin - at;
-      const int hk = (int)(off / (c > 0 ? c : 1));
-      int64_t rest = off - hk * c;
-      const SeqRows r = rows_of(b);
-      const int n_tiles = tiles_of(r);
-      for (int k0 = 0; k0 < n_tiles; k0 += kWave) {
-        int from, to;
-        const uint32_t cnt = k0 + lane0 < n_tiles ? (uint32_t)steps_of(r, k0 + lane0, from, to) : 0u;
-        uint32_t upto = cnt;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) { const uint32_t x = __shfl_up(upto, o); if (lane0 >= o) upto += x; }
-        const uint64_t past = __ballot((int64_t)upto > rest);
-        if (past) {
-          if (lane0 == __builtin_ctzll(past)) { lds.begin[0] = b; lds.begin[1] = hk; lds.begin[2] = k0 + lane0; lds.begin[3] = (int)(rest - (upto - cnt)); }
-          break;
-        }
-        rest -= __shfl(upto, 63);
-      }
-    }
-    __syncthreads();
-  }
-  int b = __builtin_amdgcn_readfirstlane(lds.begin[0]), hk = __builtin_amdgcn_readfirstlane(lds.begin[1]), tile = __builtin_amdgcn_readfirstlane(lds.begin[2]),
-      skip = __builtin_amdgcn_readfirstlane(lds.begin[3]);        // steps of the first row tile that are others'
+  const Line<ROWS, NW> line{a, plan};
+  Part part;
+  if (!line.find(lds.line, by_G, part)) return;
+  const int me = part.me;
+  const int64_t share = part.share, end = part.end;
+  int b = part.b, hk = part.hk, tile = part.tile, skip = part.skip;
 
-  for (int64_t at = begin; at < end;) {
+  for (int64_t at = part.begin; at < end;) {
     int tid = thread;
     asm volatile("" : "+v"(tid));                              // (what follows from it is not to be kept in registers from one row tile to the next)
     const int lane = tid & 63, col = lane & 31, half = lane >> 5;
-    const SeqRows r = rows_of(b);
-    const int n_tiles = tiles_of(r);
+    const SeqRows r = line.rows_of(b);
+    const int n_tiles = line.tiles_of(r);
     if (tile >= n_tiles) {                                     // the next KV head or sequence (one with rows follows: at < end <= total)
       tile = 0;
       if (n_tiles == 0 || ++hk == p.H_kv) { hk = 0; if (++b >= p.B) return; }
       continue;
     }
     int from, to;
-    const int steps = steps_of(r, tile, from, to);
+    const int steps = line.steps_of(r, tile, from, to);
     const int todo = (int)(end - at < steps - skip ? end - at : steps - skip);
     const int64_t tile_at = at - skip;
     const int k0 = skip > kStart ? skip - kStart : 0, k1 = skip + todo - kStart;   // its tiles of positions here
@@ -458,7 +341,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     const int64_t tile_end = tile_at + steps;
     bool write = true;
     if (k0 != 0 || k1 != steps - kStart) {
-      const int first_wg = k0 == 0 ? me : (int)((tile_at + kStart) / share), last_wg = tile_end <= end ? me : (int)((tile_end - 1) / share);
+      const int first_wg = k0 == 0 ? me : quotient(tile_at + kStart, share), last_wg = tile_end <= end ? me : quotient(tile_end - 1, share);
       constexpr int SLOT = NTH * (DH / 2 + 4);                 // floats: a lane's DH / 2 numerators, its maximum and its part of the denominator
       auto slot_of = [&](int wg) { return partials + ((size_t)wg * 2 + (wg == first_wg ? 1 : 0)) * SLOT; };
       auto store = [&](float* dst) {

@@ -65,6 +65,9 @@ template <int X, int N> __device__ __forceinline__ float query_to_half(uint4 (&q
   return __uint_as_float((uint32_t)(127 - lift) << 23);
 }
 
+// n / d for results that fit an int (64-bit divisions are long)
+__device__ __forceinline__ int quotient(int64_t n, int64_t d) { return n <= UINT32_MAX && d <= UINT32_MAX ? (int)((uint32_t)n / (uint32_t)d) : (int)(n / d); }
+
 // The positions [lo, hi) that row t of a sequence sees.  Both rise with t.
 struct Seen { int lo, hi; };
 __device__ __forceinline__ Seen seen_by(const PagedAttendArgs& a, const SeqRows& r, int t) {

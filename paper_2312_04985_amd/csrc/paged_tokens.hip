@@ -42,9 +42,6 @@ template <int KL, int PT> struct Stage {
   float4 sk[2], sv[2];
 };
 
-// n / d for results that fit an int (64-bit divisions are long)
-__device__ __forceinline__ int quotient(int64_t n, int64_t d) { return n <= UINT32_MAX && d <= UINT32_MAX ? (int)((uint32_t)n / (uint32_t)d) : (int)(n / d); }
-
 template <class T, int PT, int DH, int NT>
 __global__ __launch_bounds__(TT, tokens_per_cu(DH, 16 * NT)) void paged_tokens(const PagedAttendArgs a, const int max_rows, const int G, const Divider by_G, float* partials, int32_t* tickets) {
   using E = Product<T, PT>;
