@@ -93,7 +93,8 @@ constexpr int kTokensWorkgroups = 512;                  // at most
 
 // Many rows per (sequence, KV head): row tiles of chunk_rows rows.
 constexpr int chunk_rows = 128;
-constexpr int chunk_per_cu(int d_h) { return d_h == 256 ? 1 : 2; }
+// Workgroups per CU: what the registers of a wave with d_h sums per row allow.
+constexpr int chunk_per_cu(int d_h) { return d_h == 256 ? 1 : (d_h == 64 ? 3 : 2); }
 struct ChunkPlan {
   int workgroups;
   int tiles;                                            // row tiles per (sequence, KV head), each by a workgroup of its own; 0: equal parts of the work

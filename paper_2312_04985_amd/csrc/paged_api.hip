@@ -85,20 +85,26 @@ int tokens_workgroups(const sparq_paged_shape* s, int tile) {
   return (int)(want < most ? want : most);
 }
 
-// Row tiles of the second kernel per (sequence, KV head) if a workgroup serves each, 0 if they are cut into equal parts of the work:
-// where the host cannot know how many there are, and where they are fewer than three quarters of the workgroups that run at once (measured in
-// paged_chunk.hip).
+// Row tiles of the second kernel per (sequence, KV head) if a workgroup serves each, 0 if they are cut into equal parts of the work: where the host
+// cannot know how many there are, and where they are fewer than three quarters of the workgroups that run at once (128 and 256 channels), or than
+// four per CU (64; both sides are in paged_chunk.hip).
 int chunk_tiles(const sparq_paged_shape* s, int n, bool counted) {
   const int64_t rows = (int64_t)n * (s->H / s->H_kv), tiles = (rows + chunk_rows - 1) / chunk_rows;
-  return !counted && tiles * s->B * s->H_kv * 4 >= (int64_t)3 * 256 * chunk_per_cu(s->d_h) ? (int)tiles : 0;
+  const int64_t enough = s->d_h == 64 ? 4 * 256 : 3 * 256 * chunk_per_cu(s->d_h) / 4;
+  return !counted && tiles * s->B * s->H_kv >= enough ? (int)tiles : 0;
 }
 
 // Workgroups of the second kernel for equal parts: what runs at once, and no more than could have work (a row tile, and 4 tiles of positions of one).
+// With 64 channels three fit a CU; where little falls to each, two do it sooner, because fewer results are put together (us, two / three: 512 rows of
+// 4 heads over 32 768 positions, 8 KV heads, 16 bits 215 / 207, e4m3 270 / 256; up to 301 rows of 8 heads that see 1000 positions, 8 sequences
+// of 2 KV heads, int8 34.5 / 37).
 int chunk_workgroups(const sparq_paged_shape* s, int n) {
   const int64_t rows = (int64_t)n * (s->H / s->H_kv), bound = s->S_bound > 0 ? s->S_bound : (int64_t)s->max_pages * s->page_size;
-  const int64_t tiles = (int64_t)s->B * s->H_kv * ((rows + chunk_rows - 1) / chunk_rows), most = 256 * chunk_per_cu(s->d_h);
-  const int64_t could = tiles * (bound / 256 + 1);
-  return (int)(could < most ? could : most);
+  const int64_t tiles = (int64_t)s->B * s->H_kv * ((rows + chunk_rows - 1) / chunk_rows);
+  const int64_t seen = s->window > 0 && s->window + (int64_t)chunk_rows < bound ? s->window + (int64_t)chunk_rows : bound;   // positions of a row tile, at most
+  const int64_t could = tiles * (seen / 256 + 1);
+  const int per_cu = chunk_per_cu(s->d_h) > 2 && could < 4 * 3 * 256 ? 2 : chunk_per_cu(s->d_h);
+  return (int)(could < 256 * per_cu ? could : 256 * per_cu);
 }
 
 // Scratch behind the control block; the two kernels of a call follow each other and share it.

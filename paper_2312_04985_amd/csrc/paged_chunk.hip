@@ -17,9 +17,17 @@
 // Otherwise the work of the whole batch is one line of (sequence, KV head, row tile, tile of 64 positions) in order, cut into equal
 // parts, one per workgroup: chunks of different lengths and few rows over a long cache load the chip evenly as well.  A row tile
 // that several workgroups share is put together by the last of them to finish.
-// us, row tiles / the line (128 channels, f16; row tiles of all KV heads): 32 heads of 512 rows behind 8192 positions, 256 row tiles 216 / 194,
+// us, row tiles / the line, 16 bits (row tiles of all KV heads): 128 channels, 32 heads of 512 rows behind 8192 positions, 256 row tiles 216 / 194,
 // 384 278 / 311, 512 318 / 321, 640 474 / 515, 768 514 / 592, 1024 642 / 732, 1536 914 / 1117; prompts of 1024, 2048, 4096 and 8192, 256 35.5 / 40,
-// 512 75.6 / 71, 1024 212 / 215, 2048 622 / 680; 8 KV heads of 4 heads, prompts of 4096, 1024 162 / 180.
+// 512 75.6 / 71, 1024 212 / 215, 2048 622 / 680; 8 KV heads of 4 heads, prompts of 4096, 1024 162 / 180.  64 channels behind 8192 positions, 256 134 / 108,
+// 384 178 / 151, 512 191 / 187, 640 227 / 223, 1024 299 / 298; prompts, 512 51 / 44, 640 62 / 61, 1024 126 / 125, 2048 400 / 415; 8 KV heads of 4
+// heads 1024 110 / 128; 1024 of int8 pages 420 / 371 behind 8192 positions, 156 / 171 with the 8 KV heads.
+//
+// What bounds it: a prompt of 8192 (32 heads of 128 channels, f16) takes 585 us, 0.94 PFLOP/s, of which a large library product of the same
+// numbers reaches 1.31.  The matrix instructions fill 54 % of the SIMDs' cycles: two waves share a SIMD, and while the tile's reads, exponents and roundings
+// of one overlap with the products of the other, their turns do not always meet; LDS has no bank conflicts.  The clock is 1.8 GHz of 2.4 under this load
+// (zeros instead of numbers run faster), so that whatever fills the SIMDs better gains less than its share.  512 rows over 32 768 positions (8 KV heads
+// of 4 heads, bf16): 295 us, 0.92 PFLOP/s.
 #include "paged_tiles.h"
 
 namespace sparq {
@@ -31,10 +39,9 @@ template <class T, int PT, int DH>
 __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(const PagedAttendArgs a, const ChunkPlan plan, const Divider by_G) {
   using E = Product<T, PT>;
   constexpr int NW = kWaves, NTH = NW * 64, ROWS = NW * 32, PIECES = DH / 8, ND = DH / 32;
-  constexpr int GW = NW / 4;                                   // waves that load one group of 16 positions
-  constexpr int LOADS = 16 * PIECES / 64 / GW;                 // 16-bit pages: loads of 1 KB per wave, keys and values each
-  constexpr int CL = PT == kPages16 ? 1 : (DH / 64 / GW > 0 ? DH / 64 / GW : 1);   // 8-bit pages: loads of 16 codes per lane
-  static_assert(NW == 4 || (NW == 8 && DH >= 128), "whole loads");
+  constexpr int LOADS = 16 * PIECES / 64;                      // 16-bit pages: loads of 1 KB per wave, keys and values each
+  constexpr int CL = PT == kPages16 ? 1 : DH / 64;             // 8-bit pages: loads of 16 codes per lane
+  static_assert(NW * 16 == kTile, "a wave loads 16 positions of a tile");
   // One object: of several, the compiler lets reads of one wait for loads into another.
   struct Lds {
     uint16_t Kt[2][kTile * DH], Vt[2][kTile * DH];
@@ -106,10 +113,9 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
 
     // ---- loads: a wave's part of a tile is 16 positions, which share a page ----
     const int p_begin = from + k0 * kTile, p_end = from + k1 * kTile < to ? from + k1 * kTile : to;
-    const int group = wave / GW, part = wave % GW;
     // The pages of the next 64 tiles' parts, one per lane: a tile's loads do not wait for a page's.
     int pages = 0, pages_from = 0;
-    auto part_at = [&](int p0) { const int x = p0 + group * 16; return x < to ? x : from; };   // (behind the last position: any row, its values are not used)
+    auto part_at = [&](int p0) { const int x = p0 + wave * 16; return x < to ? x : from; };   // (behind the last position: any row, its values are not used)
     auto load_pages = [&](int p0) {
       pages_from = p0;
       pages = page_at(p, b, divided(part_at(lane < (to - p0) / kTile + 1 ? p0 + lane * kTile : p0), p.by_page));
@@ -128,7 +134,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
         const char* vp = reinterpret_cast<const char*>(p.V) + row * (DH * 2);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-          const int first = (part * LOADS + i) * 64, e = first + lane, rr = group * 16 + e / PIECES, slot = e % PIECES, at8 = (group * 16 * PIECES + first) * 8;
+          const int first = i * 64, e = first + lane, rr = wave * 16 + e / PIECES, slot = e % PIECES, at8 = (wave * 16 * PIECES + first) * 8;
           load_to_lds(kp, (uint32_t)((e / PIECES) * (DH * 2) + (slot ^ key_turn<DH>(rr)) * 16), &lds.Kt[buf][at8]);
           load_to_lds(vp, (uint32_t)((e / PIECES) * (DH * 2) + (slot ^ value_turn<DH>(rr)) * 16), &lds.Vt[buf][at8]);
         }
@@ -137,11 +143,12 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
         const uint8_t* vp = reinterpret_cast<const uint8_t*>(p.V) + row * DH;
 #pragma unroll
         for (int i = 0; i < CL; ++i) {
-          const int e = (part * CL + i) * 64 + lane;           // 16 codes each
+          const int e = i * 64 + lane;                         // 16 codes each
           ck[i] = *reinterpret_cast<const uint4*>(kp + e * 16);
           cv[i] = *reinterpret_cast<const uint4*>(vp + e * 16);
         }
-        if (part == 0) { csk = p.K_scale[row + (lane & 15)]; csv = p.V_scale[row + (lane & 15)]; }
+        csk = p.K_scale[row + (lane & 15)];
+        csv = p.V_scale[row + (lane & 15)];
       }
     };
     auto settle = [&](int p0, int buf) {                       // 8-bit pages: codes that have arrived go to LDS as fp16
@@ -153,16 +160,16 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
         };
 #pragma unroll
         for (int i = 0; i < CL; ++i) {
-          const int e = (part * CL + i) * 64 + lane, rr = group * 16 + e / (DH / 16), piece = e % (DH / 16) * 2;
+          const int e = i * 64 + lane, rr = wave * 16 + e / (DH / 16), piece = e % (DH / 16) * 2;
           put(&lds.Kt[buf][key_piece<DH>(rr, piece)], &lds.Kt[buf][key_piece<DH>(rr, piece + 1)], ck[i], true);
           put(&lds.Vt[buf][value_piece<DH>(rr, piece)], &lds.Vt[buf][value_piece<DH>(rr, piece + 1)], cv[i], p0 + rr < to);
         }
-        if (part == 0 && lane < 16) {
+        if (lane < 16) {
           const float v = value_scale(csv);
-          lds.s_k[buf][group * 16 + lane] = csk * c;
-          lds.s_log[buf][group * 16 + lane] = log2_normal(v);
+          lds.s_k[buf][wave * 16 + lane] = csk * c;
+          lds.s_log[buf][wave * 16 + lane] = log2_normal(v);
           // (a scale that is no number makes NaN of what sees it by its logarithm; its inverse must leave the 0 of what does not)
-          lds.s_inv[buf][group * 16 + lane] = v < INFINITY ? 1.0f / v : 0.0f;
+          lds.s_inv[buf][wave * 16 + lane] = v < INFINITY ? 1.0f / v : 0.0f;
         }
       }
     };
