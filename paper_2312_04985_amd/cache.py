@@ -64,13 +64,15 @@ class DecodeCache:
     def prefill(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, n_new_per_seq: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None, stream=None):
         """Append rows k_new, v_new [B, H_kv, n, d_h] and attend with their queries q [B, H, n, d_h] (any order with contiguous channels) over all
-        cached rows, causally: a prompt, or the next chunk of one.  The attention is sparq_paged_attention's; K and V are pages of S_max positions to it."""
+        cached rows, causally: a prompt, or the next chunk of one.  The attention is sparq_paged_attention's; K and V are pages of S_max positions to it
+        (S_max a multiple of 16, d_h 64, 128 or 256).  Outside of captures at first: it makes a workspace."""
         if self.tiled:
             raise ValueError("the tiled key layout has no rows for the attention of a chunk")
         if self._paged is None:
-            from .paged import PagedCache
-            pages = torch.arange(self.B, dtype=torch.int32, device=self.device)[:, None]
-            self._paged = PagedCache.over(self.K, self.V, pages, self.seq_lens, self.H, self.dtype)
+            from .paged import PagedCache, on_stream
+            with on_stream(stream):
+                pages = torch.arange(self.B, dtype=torch.int32, device=self.device)[:, None]
+                self._paged = PagedCache.over(self.K, self.V, pages, self.seq_lens, self.H, self.dtype)
         self.append(k_new, v_new, n_new_per_seq, stream)
         return self._paged.with_lengths(self.seq_lens).attend(q, n_new_per_seq, out=out, stream=stream)
 

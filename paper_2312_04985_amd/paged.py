@@ -4,6 +4,7 @@ Allocation and bookkeeping only (torch owns the memory); all work is done by lib
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
 from typing import Optional, Union
 
 import torch
@@ -13,6 +14,11 @@ from .cache import DecodeCache
 
 PAGE_TYPES = {"16": B.SPARQ_PAGES_16, "i8": B.SPARQ_PAGES_I8, "e4m3": B.SPARQ_PAGES_E4M3}
 CODE_TYPES = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+def on_stream(stream):
+    """What a call makes for itself belongs to its stream: torch fills it in order with the call's kernels."""
+    return nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class PagedCache:
@@ -65,10 +71,18 @@ class PagedCache:
         self.cache = B.make_paged_cache(K, V, K_scale, V_scale, page_table, seq_lens)
         self.shape = B.make_paged_shape(Bsz, H, H_kv, d_h, page_size, n_pages, max_pages, dtype, PAGE_TYPES[self.pages],
                                         0 if causal else B.SPARQ_FLAG_PAGED_ALL, window)
-        self.workspace = torch.zeros((B.sparq_paged_workspace_bytes(self.shape, 1),), dtype=torch.uint8, device=self.device)
+        need = B.sparq_paged_workspace_bytes(self.shape, 1)
         self._rows_room, self._outgrown = 1, []
         with torch.cuda.device(self.device):
-            B.sparq_workspace_init(self.workspace)
+            self.workspace = self._new_workspace(need, None)
+
+    def _new_workspace(self, need: int, stream) -> torch.Tensor:
+        with on_stream(stream):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a cache's workspace cannot be made during a capture: make a call of this size before it")
+            w = torch.empty((need,), dtype=torch.uint8, device=self.device)
+            B.sparq_workspace_init(w, stream)
+            return w
 
     def with_bound(self, S_bound: int) -> "PagedCache":
         """Promise that no sequence is longer than S_bound (0: what the page table has room for)."""
@@ -115,11 +129,9 @@ class PagedCache:
         """Room for calls of n rows per sequence.  The old workspace stays: calls in flight and captured ones go on using it."""
         need = B.sparq_paged_workspace_bytes(self.shape, n)
         if need > self.workspace.numel():
-            if torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("the workspace is too small for this call and cannot be replaced during a capture: make a call of this size before it")
+            w = self._new_workspace(need, stream)
             self._outgrown.append(self.workspace)
-            self.workspace = torch.empty((need,), dtype=torch.uint8, device=self.device)
-            B.sparq_workspace_init(self.workspace, stream)
+            self.workspace = w
         self._rows_room = n
 
     def _elsewhere(self, stream) -> bool:
@@ -147,7 +159,8 @@ class PagedCache:
             with torch.cuda.device(self.device):
                 return self.attend(q, n_new_per_seq, row_start, n_new, out, lse, stream)
         if out is None:          # rows that belong to no sequence are not written
-            out = torch.empty_like(q) if n_new_per_seq is None and row_start is None else torch.zeros_like(q)
+            with on_stream(stream):
+                out = torch.empty_like(q) if n_new_per_seq is None and row_start is None else torch.zeros_like(q)
         elif out.shape != q.shape or out.dtype is not q.dtype or out.device != q.device:
             raise ValueError("out must have q's shape, type and device")
         q4, o4 = (q.unsqueeze(2), out.unsqueeze(2)) if row_start is None and q.dim() == 3 else (q, out)
@@ -155,7 +168,8 @@ class PagedCache:
         lse_out = None
         if lse is not None and lse is not False:
             size = (self.H, q.shape[0]) if row_start is not None else (self.B, self.H, q4.shape[2])
-            lse_out = torch.full(size, -float("inf"), dtype=torch.float32, device=self.device) if lse is True else lse
+            with on_stream(stream):
+                lse_out = torch.full(size, -float("inf"), dtype=torch.float32, device=self.device) if lse is True else lse
             if lse_out.shape != size or lse_out.device != self.device:
                 raise ValueError(f"lse must be {size} on {self.device}")
         B.sparq_paged_attention(self.shape, self.cache, rows, q4, o4, lse_out, self.workspace, stream)

@@ -202,3 +202,45 @@ def test_a_workspace_outgrown():
     out = c.attend(x)
     assert c.workspace.numel() > small and c.error_flags() == B.SPARQ_ERR_BAD_PAGE and c.error_flags() == 0
     P.check_attention(built, q, out.transpose(1, 2), [200])
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_results_that_a_call_makes_belong_to_its_stream(packed):
+    """Outputs and logarithms made by the call on another stream are filled there, before its kernels, however busy the current one is."""
+    built = P.Built((200, 131), 4, 2, 64, "f16", "16", 16, 370).fill()
+    n = (5, 40)
+    q = built.queries(40).cuda().transpose(1, 2)
+    if packed:
+        x = torch.cat([q[b, :, :n[b]].transpose(0, 1) for b in range(2)]).contiguous()
+        kw = dict(row_start=torch.tensor([0, 5, 45], dtype=torch.int32, device="cuda"), n_new=40)
+    else:
+        x, kw = q, dict(n_new_per_seq=torch.tensor(n, dtype=torch.int32, device="cuda"))
+    want, want_lse = built.c.attend(x, lse=True, **kw)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy = torch.randn((4096, 4096), device="cuda")
+    for _ in range(20):
+        busy = busy @ busy * 1e-3
+    out, lse = built.c.attend(x, lse=True, stream=other, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_a_first_prefill_is_not_captured():
+    """It makes a workspace, which is initialised outside of a graph; after a prefill the next one may be captured."""
+    c = DecodeCache(1, 2, 2, 64, 64, 16, 16, torch.float16)
+    x = torch.randn((1, 2, 8, 64), device="cuda", dtype=torch.float16)
+    with pytest.raises(RuntimeError, match="capture"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            c.prefill(x, x, x)
+    torch.cuda.synchronize()
+    c.seq_lens.zero_()
+    a = c.prefill(x, x, x)
+    out, graph = torch.empty_like(x), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.prefill(x, x, x, out=out)
+    for _ in range(3):
+        c.seq_lens.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, a) and c.error_flags() == 0
