@@ -326,7 +326,8 @@ typedef struct {
  * (elements), or with row_start at base + head * strides.head + (row_start[b] + t) * strides.row: sequences of different lengths
  * packed one behind the other.  Rows that belong to no sequence, and those from n_b on, are neither read nor written. */
 typedef struct {
-  int32_t n;                 /* the most rows that a sequence has in this call (>= 1) */
+  int32_t n;                 /* the most rows that a sequence has in this call (>= 1).  B n H < 2^31, of appends and reads also B n H_kv d_h / 8 < 2^32 - 2^12
+                              * (SPARQ_EUNSUPPORTED): the launches are sized by it */
   int32_t n_rows;            /* with row_start: rows in the packed buffers; otherwise ignored */
   const int32_t* n_per_seq;  /* device [B], rows of each sequence (0 .. n), or NULL: n everywhere */
   const int32_t* row_start;  /* device [B + 1] or NULL; row_start[b + 1] - row_start[b] (0 .. n) is sequence b's count.  Not both. */

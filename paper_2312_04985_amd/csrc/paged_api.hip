@@ -91,7 +91,7 @@ int tokens_workgroups(const sparq_paged_shape* s, int tile) {
 int chunk_tiles(const sparq_paged_shape* s, int n, bool counted) {
   const int64_t rows = (int64_t)n * (s->H / s->H_kv), tiles = (rows + chunk_rows - 1) / chunk_rows;
   const int64_t enough = s->d_h == 64 ? 4 * 256 : 3 * 256 * chunk_per_cu(s->d_h) / 4;
-  return !counted && tiles * s->B * s->H_kv >= enough ? (int)tiles : 0;
+  return !counted && tiles * s->B * s->H_kv >= enough && tiles * s->B * s->H_kv <= UINT32_MAX / 256 ? (int)tiles : 0;   // (threads of a launch: 32 bits)
 }
 
 // Workgroups of the second kernel for equal parts: what runs at once, and no more than could have work (a row tile, and 4 tiles of positions of one).
@@ -151,6 +151,8 @@ PagedArgs paged_args(const sparq_paged_shape* s, const sparq_paged_cache* c, con
 int move_rows(const sparq_paged_shape* shape, const sparq_paged_cache* cache, const sparq_rows* rows, const int32_t* first, void* k, void* v,
               const sparq_strides* strides, void* workspace, size_t workspace_bytes, void* hip_stream, bool reads) {
   int rc = check_call(shape, cache, rows, workspace, workspace_bytes);
+  // (a thread for 8 channels, and no more than 2^32 of them)
+  if (rc == SPARQ_OK && (int64_t)shape->B * rows->n * shape->H_kv > UINT32_MAX / (shape->d_h / 8) - 256) rc = SPARQ_EUNSUPPORTED;
   if (rc == SPARQ_OK && (!k || !v || !aligned16(k) || !aligned16(v))) rc = SPARQ_EINVAL;
   if (rc == SPARQ_OK) rc = check_strides(shape, rows, strides, shape->H_kv, reads);
   if (rc != SPARQ_OK) return rc;

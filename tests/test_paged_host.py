@@ -89,6 +89,16 @@ def test_pointers_rows_strides_and_workspaces():
     assert L.sparq_paged_append(ctypes.byref(shape()), ctypes.byref(cache()), ctypes.byref(rows()), FAKE, FAKE, None, FAKE, ROOM, None) == E
 
 
+@pytest.mark.parametrize("d_h,n", [(64, 1 << 25), (128, 1 << 24), (256, 1 << 23)])
+def test_rows_beyond_a_launch(d_h, n):
+    """A thread moves 8 channels: B n H_kv d_h / 8 threads of one launch count in 32 bits."""
+    sh = shape(B=16, H=1, H_kv=1, d_h=d_h)
+    st = strides(seq=n * d_h, head=d_h, row=d_h)
+    assert 16 * n * (d_h // 8) == 1 << 32 and 16 * n < 1 << 31
+    assert calls(sh, r=rows(n), s=st, skip=("attend",), ws_bytes=1 << 60) == {B.SPARQ_EUNSUPPORTED}
+
+
+
 def test_a_workspace_serves_calls_of_fewer_rows():
     for kw in (dict(), dict(max_pages=2048, page_size=16), dict(B=64, H=32, H_kv=8, max_pages=512), dict(B=1, H=32, H_kv=1, max_pages=4096, d_h=256)):
         sizes = [B.sparq_paged_workspace_bytes(shape(**kw), n) for n in (1, 2, 7, 8, 15, 16, 17, 64, 65, 500, 4096)]
