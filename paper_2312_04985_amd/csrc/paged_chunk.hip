@@ -365,23 +365,31 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
         for (int j = 0; j < ND; ++j)
 #pragma unroll
           for (int i = 0; i < 16; ++i) O[j][i] = 0.0f;
+        constexpr int AT_ONCE = DH <= 128 ? 2 : 1;             // results in flight
 #pragma unroll 1
-        for (; wg <= to_wg; wg += step) {
-          const float* src = slot_of(wg);
-          const float4 st = load_agent4(src, (uint32_t)(ND * 4 * NTH + tid) * 16);
-          const float m_to = fmaxf(m_ref, st.x), f = weight_exp2(m_ref, m_to), g = weight_exp2(st.x, m_to);
-          m_ref = m_to;
-          l = l * f + st.y * g;
+        for (; wg <= to_wg; wg += AT_ONCE * step) {
+          float4 st[AT_ONCE], o[AT_ONCE][ND * 4 / (3 - AT_ONCE)];
+          auto fetch = [&](int i, int q0) {
+            const float* src = slot_of(wg + i * step <= to_wg ? wg + i * step : wg);
+            if (q0 == 0) st[i] = load_agent4(src, (uint32_t)(ND * 4 * NTH + tid) * 16);
 #pragma unroll
-          for (int j = 0; j < ND; j += 2) {
-            float4 o[8];
+            for (int q = 0; q < ND * 4 / (3 - AT_ONCE); ++q) o[i][q] = load_agent4(src, (uint32_t)((q0 + q) * NTH + tid) * 16);
+          };
 #pragma unroll
-            for (int q = 0; q < 8; ++q) o[q] = load_agent4(src, (uint32_t)((j * 4 + q) * NTH + tid) * 16);
+          for (int i = 0; i < AT_ONCE; ++i) fetch(i, 0);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              f32x16& x = O[j + q / 4];
+          for (int i = 0; i < AT_ONCE; ++i) {
+            if (wg + i * step > to_wg) break;
+            const float m_to = fmaxf(m_ref, st[i].x), f = weight_exp2(m_ref, m_to), g = weight_exp2(st[i].x, m_to);
+            m_ref = m_to;
+            l = l * f + st[i].y * g;
+#pragma unroll
+            for (int q = 0; q < ND * 4; ++q) {
+              if (q > 0 && q % (ND * 4 / (3 - AT_ONCE)) == 0) fetch(i, q);
+              f32x16& x = O[q / 4];
+              const float4& y = o[i][q % (ND * 4 / (3 - AT_ONCE))];
               const int e = q % 4 * 4;
-              x[e] = x[e] * f + o[q].x * g; x[e + 1] = x[e + 1] * f + o[q].y * g; x[e + 2] = x[e + 2] * f + o[q].z * g; x[e + 3] = x[e + 3] * f + o[q].w * g;
+              x[e] = x[e] * f + y.x * g; x[e + 1] = x[e + 1] * f + y.y * g; x[e + 2] = x[e + 2] * f + y.z * g; x[e + 3] = x[e + 3] * f + y.w * g;
             }
           }
         }
