@@ -82,11 +82,14 @@ __host__ __device__ inline int64_t pool_row(const PagedArgs& a, int page, int he
 // Few rows per (sequence, KV head): the launch's workgroups and what they leave for each other.
 struct TokensPlan {
   int workgroups, max_rows;                             // max_rows: tokens times group, 0: no sequence is served that way
-  float* partials;                                      // [workgroups][2][16, 32 or 64][d_h + 4]
+  float* partials;                                      // [workgroups][2][16 or 32][d_h + 4]
   int32_t* tickets;                                     // [workgroups], 0 between launches
 };
-// The most rows that a workgroup's registers hold next to the positions in flight.
-constexpr int tokens_rows(int d_h) { return d_h == 64 ? 64 : (d_h == 128 ? 32 : 16); }
+// The most rows, tokens times group, for which it is faster than the other kernel, or whose sums registers hold next to the positions in flight (us, this
+// kernel / the other; f16 rows of 8 KV heads over 32 768 positions: 16 bits, 64 channels, 4 rows 19.5 / 35, 32 31.5 / 35, 40 43 / 37, 64 50 / 38; 128
+// channels, 4 and 32 rows 32 / 55 and 53 / 56; 256 channels, 4 and 16 rows 57 / 103 and 76 / 103; int8 pages, 64 channels, 32 and 40 rows 33 / 39 and 45 / 41;
+// 16 sequences of 4096 positions, 128 channels, 4 rows 53 / 63, of int8 pages 23 / 43).
+constexpr int tokens_rows(int d_h) { return d_h == 256 ? 16 : 32; }
 // Workgroups per CU by what they are built for: with 4096 sums a wave's registers are those of two.
 constexpr int tokens_per_cu(int d_h, int tile_rows) { return d_h * tile_rows >= 4096 ? 1 : 2; }
 constexpr int kTokensWorkgroups = 512;                  // at most

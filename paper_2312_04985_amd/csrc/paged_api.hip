@@ -61,8 +61,8 @@ int check_paged_cache(const sparq_paged_shape* s, const sparq_paged_cache* c) {
   return SPARQ_OK;
 }
 
-// How an attention call is served: by the kernel whose waves divide the positions where all rows of a KV head (tokens times
-// group) fit one workgroup's registers, by the kernel whose waves divide the rows otherwise; by both where only the
+// How an attention call is served: by the kernel whose waves divide the positions where the rows of a KV head (tokens times
+// group) are few (tokens_rows), by the kernel whose waves divide the rows otherwise; by both where only the
 // device knows how many rows each sequence has: single tokens then go to the first, longer chunks to the second.
 struct AttendPlan { int tokens_rows, chunk; };   // rows that the first kernel takes at most (0: not launched); whether the second is launched
 
@@ -74,7 +74,7 @@ AttendPlan attend_plan(const sparq_paged_shape* s, int n, bool counted) {
   return {single <= most ? (int)single : 0, 1};
 }
 
-int tokens_tile(int rows) { return rows <= 16 ? 16 : (rows <= 32 ? 32 : 64); }
+int tokens_tile(int rows) { return rows <= 16 ? 16 : 32; }
 
 // Workgroups of the first kernel: what runs at once, but no more than 32 for a unit, whose last one puts their results together, or 64 while
 // that keeps to one per CU (us, 32 / 64 for each, 32 768 positions of 128 channels: 8 units of e4m3 pages 25.2 / 28.3, of 16 bits 32.3 / 36.0;
