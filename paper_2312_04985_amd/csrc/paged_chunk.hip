@@ -15,8 +15,8 @@
 // Two ways to divide the work.  Where the host knows that there are row tiles enough, a workgroup serves one of them; the
 // dispatcher levels their sizes out, and the workgroups of a KV head, which read the same rows, run next to each other on one XCD.
 // Otherwise the work of the whole batch is one line of (sequence, KV head, row tile, tile of 64 positions) in order, cut into equal
-// parts, one per workgroup: chunks of different lengths and few rows over a long cache load the chip evenly as well.  A row tile
-// that several workgroups share is put together by the last of them to finish.
+// parts, one per workgroup: chunks of different lengths and few rows over a long cache load the chip evenly as well; where the lengths allow it, the
+// cuts are those of row tiles into parts of their own.  A row tile that several workgroups share is put together by the last of them to finish.
 // us, row tiles / the line, 16 bits (row tiles of all KV heads): 128 channels, 32 heads of 512 rows behind 8192 positions, 256 row tiles 216 / 194,
 // 384 278 / 311, 512 318 / 321, 640 474 / 515, 768 514 / 592, 1024 642 / 732, 1536 914 / 1117; prompts of 1024, 2048, 4096 and 8192, 256 35.5 / 40,
 // 512 75.6 / 71, 1024 212 / 215, 2048 622 / 680; 8 KV heads of 4 heads, prompts of 4096, 1024 162 / 180.  64 channels behind 8192 positions, 256 134 / 108,
@@ -27,7 +27,7 @@
 // numbers reaches 1.31.  The matrix instructions fill 54 % of the SIMDs' cycles: two waves share a SIMD, and while the tile's reads, exponents and roundings
 // of one overlap with the products of the other, their turns do not always meet; LDS has no bank conflicts.  The clock is 1.8 GHz of 2.4 under this load
 // (zeros instead of numbers run faster), so that whatever fills the SIMDs better gains less than its share.  512 rows over 32 768 positions (8 KV heads
-// of 4 heads, bf16): 295 us, 0.92 PFLOP/s.
+// of 4 heads, bf16): 275 us, 0.99 PFLOP/s.
 #include "paged_tiles.h"
 
 namespace sparq {
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(kWaves * 64, chunk_per_cu(DH)) void paged_chunk(con
     const int64_t tile_end = tile_at + steps;
     bool write = true;
     if (k0 != 0 || k1 != steps - kStart) {
-      const int first_wg = k0 == 0 ? me : quotient(tile_at + kStart, share), last_wg = tile_end <= end ? me : quotient(tile_end - 1, share);
+      const int first_wg = share == 0 ? part.first : (k0 == 0 ? me : quotient(tile_at + kStart, share)), last_wg = share == 0 ? part.last : (tile_end <= end ? me : quotient(tile_end - 1, share));
       constexpr int SLOT = NTH * (DH / 2 + 4);                 // floats: a lane's DH / 2 numerators, its maximum and its part of the denominator
       auto slot_of = [&](int wg) { return partials + ((size_t)wg * 2 + (wg == first_wg ? 1 : 0)) * SLOT; };
       auto store = [&](float* dst) {

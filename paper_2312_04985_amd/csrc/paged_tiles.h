@@ -47,8 +47,9 @@ __device__ __forceinline__ void tile_barrier() {
 // nothing are written too), behind kStart that stand for its start and end.
 template <int NW> struct LineLds { int64_t sum_w[NW]; int begin[4]; };
 // A workgroup's part: [begin, end) of the line, whose first step is step `skip` of row tile `tile` of (sequence b, KV head hk); with `plan.tiles` one
-// row tile whole.  `share`: steps per workgroup, of which this is number `me`.
-struct Part { int64_t begin, end, share; int me, b, hk, tile, skip; };
+// row tile whole.  `share`: steps per workgroup, of which this is number `me`; 0 where a row tile is cut into parts of its own, which the
+// workgroups `first` to `last` have.
+struct Part { int64_t begin, end, share; int me, b, hk, tile, skip, first, last; };
 
 template <int ROWS, int NW> struct Line {
   const PagedAttendArgs& a;
@@ -69,11 +70,16 @@ template <int ROWS, int NW> struct Line {
     to = seen_by(a, r, divided(m1 - 1, a.by_group)).hi;
     return kStart + (to - from <= kTile ? 1 : (to - from + kTile - 1) / kTile);
   }
-  __device__ __forceinline__ int64_t steps_of_unit(const SeqRows& r, int lane) const {   // by all lanes of a wave together
+  // ... of `size` steps or a rest of them
+  __device__ __forceinline__ int parts_of(const SeqRows& r, int k, int size) const {
+    int from, to;
+    const int steps = steps_of(r, k, from, to);
+    return size == 1 ? steps : (int)((uint32_t)(steps + size - 1) / (uint32_t)size);
+  }
+  __device__ __forceinline__ int64_t parts_of_unit(const SeqRows& r, int size, int lane) const {   // by all lanes of a wave together
     const int n_tiles = tiles_of(r);
     int64_t sum = 0;
-    int from, to;
-    for (int k = lane; k < n_tiles; k += kWave) sum += steps_of(r, k, from, to);
+    for (int k = lane; k < n_tiles; k += kWave) sum += parts_of(r, k, size);
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o);
     return sum;
@@ -99,30 +105,49 @@ template <int ROWS, int NW> struct Line {
       part.end = steps_of(r, part.tile, from, to);
       return true;
     }
-    // Consecutive parts of the line share rows of the cache; so that they share an L2 too, each XCD takes an eighth of the line.
-    if (G % 8 == 0) part.me = (int)(blockIdx.x % 8) * (G / 8) + (int)blockIdx.x / 8;
     const int per = (p.B + NW - 1) / NW, b_first = wave * per, b_last = b_first + per < p.B ? b_first + per : p.B;
-    int64_t mine = 0;
-    for (int b = b_first; b < b_last; ++b) {
-      const SeqRows r = rows_of(b);
-      if (r.err && part.me == 0 && lane == 0) atomicOr(p.err, r.err);
-      mine += steps_of_unit(r, lane);
-    }
-    if (lane == 0) lds.sum_w[wave] = mine;
-    __syncthreads();
-    int64_t before = 0, total = 0;
+    int64_t mine, before, total;
+    auto count = [&](int size) {
+      mine = 0;
+      for (int b = b_first; b < b_last; ++b) mine += parts_of_unit(rows_of(b), size, lane);
+      if (lane == 0) lds.sum_w[wave] = mine;
+      __syncthreads();
+      before = 0; total = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) { before += w < wave ? lds.sum_w[w] : 0; total += lds.sum_w[w]; }
-    before *= p.H_kv; total *= p.H_kv;
+      for (int w = 0; w < NW; ++w) { before += w < wave ? lds.sum_w[w] : 0; total += lds.sum_w[w]; }
+      before *= p.H_kv; total *= p.H_kv;
+      __syncthreads();
+    };
+    if (blockIdx.x == 0)
+      for (int b = b_first; b < b_last; ++b) { const int err = rows_of(b).err; if (err && lane == 0) atomicOr(p.err, err); }
+    count(1);
     part.share = total < INT32_MAX - G ? (int64_t)divided((int)total + G - 1, by_G) : (total + G - 1) / G;
-    part.begin = (int64_t)part.me * part.share;
-    part.end = part.begin + part.share < total ? part.begin + part.share : total;
-    if (part.begin >= part.end) return false;
+    // Where the workgroups can be dealt out to the row tiles, each cut into equal parts of at most 9/8 of a share, they are: those of a KV head then go
+    // through the same positions at the same time and find them in their L2.  us, shares of the line / such parts, 16 bits, 8 KV heads of 4 heads of 128
+    // channels: 512 rows over 32 768 positions (128 row tiles, 4 parts each) 345 / 321, 256 rows 186 / 166, 512 over 20 000 204 / 199; 32 heads of
+    // 512 rows over 8192 183 / 185, 4 sequences of 256 rows over 8192 192 / 184.
+    int size = 1;
+    if (part.share >= 8 && part.share < INT32_MAX / 2) {
+      const int64_t keep_mine = mine, keep_before = before, keep_total = total;
+      size = (int)part.share + (int)part.share / 8;
+      count(size);
+      if (total > G) { size = 1; mine = keep_mine; before = keep_before; total = keep_total; }
+      else part.share = 0;
+    }
+    // Consecutive parts share rows of the cache; so that they share an L2 too, each XCD takes an eighth of them.
+    const int used = size == 1 ? G : (int)total, eighth = (used + 7) / 8;
+    if (G % 8 == 0) {
+      if ((int)blockIdx.x / 8 >= eighth) return false;
+      part.me = (int)(blockIdx.x % 8) * eighth + (int)blockIdx.x / 8;
+    }
+    part.begin = size == 1 ? (int64_t)part.me * part.share : part.me;
+    part.end = size == 1 && part.begin + part.share < total ? part.begin + part.share : total;
+    if (part.begin >= total) return false;
     if (before <= part.begin && part.begin < before + mine * p.H_kv) {   // one wave
       int64_t at = before, c = 1;
       int b = b_first;
       for (; b < b_last; ++b) {
-        c = steps_of_unit(rows_of(b), lane);
+        c = parts_of_unit(rows_of(b), size, lane);
         if (part.begin < at + c * p.H_kv || b == b_last - 1) break;
         at += c * p.H_kv;
       }
@@ -132,8 +157,7 @@ template <int ROWS, int NW> struct Line {
       const SeqRows r = rows_of(b);
       const int n_tiles = tiles_of(r);
       for (int k0 = 0; k0 < n_tiles; k0 += kWave) {
-        int from, to;
-        const uint32_t cnt = k0 + lane < n_tiles ? (uint32_t)steps_of(r, k0 + lane, from, to) : 0u;
+        const uint32_t cnt = k0 + lane < n_tiles ? (uint32_t)parts_of(r, k0 + lane, size) : 0u;
         uint32_t upto = cnt;
 #pragma unroll
         for (int o = 1; o < kWave; o <<= 1) { const uint32_t x = __shfl_up(upto, o); if (lane >= o) upto += x; }
@@ -148,6 +172,17 @@ template <int ROWS, int NW> struct Line {
     __syncthreads();
     part.b = __builtin_amdgcn_readfirstlane(lds.begin[0]); part.hk = __builtin_amdgcn_readfirstlane(lds.begin[1]);
     part.tile = __builtin_amdgcn_readfirstlane(lds.begin[2]); part.skip = __builtin_amdgcn_readfirstlane(lds.begin[3]);
+    if (size > 1) {                                            // part `skip` of the row tile
+      int from, to;
+      const int mine_is = part.skip, steps = steps_of(rows_of(part.b), part.tile, from, to), tiles = steps - kStart;
+      const int parts = (int)((uint32_t)(steps + size - 1) / (uint32_t)size), each = (tiles + parts - 1) / parts, needed = (tiles + each - 1) / each;
+      if (mine_is >= needed) return false;
+      part.first = part.me - mine_is;
+      part.last = part.first + needed - 1;
+      part.skip = mine_is ? kStart + mine_is * each : 0;
+      part.begin = part.skip;
+      part.end = kStart + (mine_is + 1) * each < steps ? kStart + (mine_is + 1) * each : steps;
+    }
     return true;
   }
 };

@@ -174,6 +174,28 @@ def test_few_rows_over_a_long_cache(d_h, g, n, dtype, pages):
         assert torch.equal(again, out) and torch.equal(lse2, lse)
 
 
+@pytest.mark.parametrize("d_h,h_kv,g,dtype,pages,lens,counts,window", [
+    (128, 2, 4, "f16", "16", (20011,), (500,), 0),            # 16 row tiles per KV head, 15 parts each
+    (128, 2, 4, "bf16", "e4m3", (20011, 9007), (300, 200), 0),   # ... of different lengths
+    (256, 1, 2, "f16", "16", (20011,), (1500,), 8000),
+    (64, 3, 4, "bf16", "i8", (20011,), (440,), 0)])
+def test_row_tiles_in_parts_of_their_own(d_h, h_kv, g, dtype, pages, lens, counts, window):
+    """Chunks over long caches whose row tiles the workgroups are dealt out to in equal parts; the same bits every time."""
+    built = P.Built(lens, h_kv * g, h_kv, d_h, dtype, pages, 64, 345, window=window).fill()
+    n = max(counts)
+    q = built.queries(n)
+    x = q.cuda().transpose(1, 2)
+    kw = {} if len(lens) == 1 else dict(n_new_per_seq=torch.tensor(counts, dtype=torch.int32, device="cuda"))
+    out, lse = torch.full_like(x, 7), torch.full(x.shape[:3], 7.0, device="cuda")       # (rows behind a sequence's last stay as they are)
+    built.c.attend(x, out=out, lse=lse, **kw)
+    P.check_attention(built, q, out.transpose(1, 2), list(counts), lse, window=window)
+    for _ in range(3):
+        again, lse2 = torch.full_like(x, 7), torch.full(x.shape[:3], 7.0, device="cuda")
+        built.c.attend(x, out=again, lse=lse2, **kw)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+    assert built.c.error_flags() == 0
+
+
 def test_a_workspace_that_serves_calls_of_every_size():
     """Calls of few, many and few rows on one workspace: every call leaves its counters as it found them."""
     built = P.Built((3000, 900), 8, 2, 128, "bf16", "16", 64, 350).fill()
