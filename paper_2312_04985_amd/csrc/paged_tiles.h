@@ -124,7 +124,7 @@ template <int ROWS, int NW> struct Line {
     part.share = total < INT32_MAX - G ? (int64_t)divided((int)total + G - 1, by_G) : (total + G - 1) / G;
     // Where the workgroups can be dealt out to the row tiles, each cut into equal parts of at most 9/8 of a share, they are: those of a KV head then go
     // through the same positions at the same time and find them in their L2.  us, shares of the line / such parts, 16 bits, 8 KV heads of 4 heads of 128
-    // channels: 512 rows over 32 768 positions (128 row tiles, 4 parts each) 345 / 321, 256 rows 186 / 166, 512 over 20 000 204 / 199; 32 heads of
+    // channels: 512 rows over 32 768 positions (128 row tiles, 4 parts each) 345 / 321, 1273 / 176 MB fetched; 256 rows 186 / 166, 512 over 20 000 204 / 199; 32 heads of
     // 512 rows over 8192 183 / 185, 4 sequences of 256 rows over 8192 192 / 184.
     int size = 1;
     if (part.share >= 8 && part.share < INT32_MAX / 2) {
